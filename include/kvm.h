@@ -354,6 +354,47 @@ int kvm_prepare_qkv(const kvm_prep_params *p, const void *q_raw, const void *k_r
                     const void *prev_v, void *q_out, void *k_out, void *v_out, float *gate_out,
                     void *scratch, int64_t T, int64_t pos0, void *stream);
 
+/* ---- Linear attention with a decay for each KV head ----------------------------------------------
+ * A mixer that hybrids put beside the KVM layer, in the same layouts: one fp32 state S [d, d] (key channel, value
+ * channel) per sequence and KV head, whatever the tokens seen;
+ *   S_t = exp(a_h) S_{t-1} + k_t v_t^T,   out_t = scale * q_t S_t,
+ * a_h = log_decay[h] <= 0 a constant of the KV head (device fp32 [H_kv]; it gets no gradient; values above 0 are not
+ * refused, the state then grows).  The H_q / H_kv query heads of a group share one state.  Sums and states are
+ * fp32; q, k, v, out are KVM_F32 or KVM_BF16.  In prompts tokens are taken 64 at a time (fp32: 32): a NaN or an infinity of a later
+ * token's k or v, or an earlier one's, makes NaN of outputs of the same group of tokens; behind it the state is NaN where
+ * the recurrence makes it infinite or NaN.
+ * lens: nullable device int32 [B], the tokens of each sequence of a padded batch (taken as 0 .. T): rows behind are
+ * not looked at, their out is zero, and the state is the one at the sequence's own end.  Every pointer is 16-byte aligned;
+ * outputs must not overlap inputs, except that state_out may be state_in itself. */
+typedef struct kvm_linear_config {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim; /* d: 64 or 128; batch * n_q_heads < 2^24 */
+  int32_t io_dtype;                                /* KVM_F32 | KVM_BF16 */
+  float scale;                                     /* 0 selects 1 / sqrt(d) */
+} kvm_linear_config;
+
+/* Bytes of device workspace that kvm_linear_prefill and kvm_linear_backward need for T tokens (start states of the
+ * parts a sequence is cut into); 0 on bad arguments. */
+size_t kvm_linear_workspace_bytes(const kvm_linear_config *cfg, int64_t T);
+
+/* T tokens of every sequence.  q, out: [B, T, H_q, d]; k, v: [B, T, H_kv, d], strided as in kvm_prefill_chunked (NULL =
+ * dense; multiples of 16 bytes, token strides up to 2^23 elements; gate and lse strides are not looked at); state_in, state_out: fp32 [B, H_kv, d, d] or NULL (zero; not
+ * wanted).  Work is enqueued on `stream`.  Errors: KVM_ERR_ARG, KVM_ERR_CAPACITY (workspace), KVM_ERR_HIP. */
+int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, const void *k, const void *v, const float *log_decay,
+                       const float *state_in, const int32_t *lens, void *out, float *state_out, int64_t T,
+                       const kvm_strides *strides, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients of a loss with respect to q, k, v and state_in of that call (dense), from dout, the gradient with respect to its out,
+ * and dstate_out, that with respect to its state_out (NULL: none).  dstate_in may be NULL.  Rows behind a sequence get zero. */
+int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, const void *k, const void *v, const float *log_decay,
+                        const float *state_in, const int32_t *lens, const void *dout, const float *dstate_out, void *dq,
+                        void *dk, void *dv, float *dstate_in, int64_t T, void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+/* One token per sequence: the state is advanced in place and asked.  q, out: [B, H_q, d]; k, v: [B, H_kv, d], dense;
+ * active: nullable device int32 [B]; a sequence whose entry is 0 keeps its state and gets zeros. */
+int kvm_linear_decode(const kvm_linear_config *cfg, float *state, const void *q, const void *k, const void *v,
+                      const float *log_decay, const int32_t *active, void *out, void *stream);
+
 /* Measured peaks of the GPU, for rooflines (no passage of the paper: measurement aids).  Both
  * calls enqueue a microkernel on `stream`, wait for it (they block the host) and report its rate.
  *   kvm_measure_mfma_bf16_peak: 2048 workgroups x 4 waves issue `iters` x 4 independent

@@ -1,4 +1,4 @@
-"""torch.autograd front end of the layer: one differentiable call for a whole sequence.
+"""torch.autograd front end of the layer, and of the mixers beside it: one differentiable call for a whole sequence.
 
 Marshalling only.  The forward is kvm_prefill_chunked on a fresh state with the fold record
 switched on; the backward is kvm_prefill_backward on that state.  Every step runs in the
@@ -10,7 +10,7 @@ from typing import Optional
 
 import torch
 
-from .binding import KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState
+from .binding import KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, linear_backward, linear_prefill
 
 
 class _KVMAttention(torch.autograd.Function):
@@ -58,3 +58,35 @@ def kvm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gate: Optio
                budget_kind=budget_kind, budget_fixed=budget_fixed, budget_scale=budget_scale,
                budget_table=budget_table, ln_eps=ln_eps, norm_eps=norm_eps)
     return _KVMAttention.apply(q, k, v, gate, ln_gamma, ln_beta, tau_state, tau_bswa, cfg)
+
+
+class _LinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, state, lens, scale):
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        out, end = linear_prefill(q, k, v, log_decay, state=state, lens=lens, scale=scale)
+        ctx.save_for_backward(q, k, v, log_decay, state, lens)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return out, end
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dend):
+        q, k, v, log_decay, state, lens = ctx.saved_tensors
+        dout = torch.zeros_like(q) if dout is None else dout.contiguous()
+        dend = None if dend is None else dend.contiguous()
+        dq, dk, dv, dstate = linear_backward(q, k, v, log_decay, dout, state=state, dstate_out=dend, lens=lens, scale=ctx.scale,
+                                             want_dstate=state is not None and ctx.needs_input_grad[4])
+        return dq, dk, dv, None, dstate, None, None
+
+
+def kvm_linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, *,
+                         state: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None,
+                         scale: Optional[float] = None):
+    """Linear attention with a decay for each KV head over a whole sequence, differentiable in q, k, v and the state it
+    starts from: S_t = exp(log_decay) S_{t-1} + k_t v_t^T, out_t = scale q_t S_t.  Shapes and lens as in linear_prefill.  The decays
+    are constants of the layer: a log_decay that requires a gradient is refused.  Returns (out, state behind the last token)."""
+    if log_decay.requires_grad:
+        raise ValueError("log_decay: the decays are constants, they get no gradient")
+    return _LinearAttention.apply(q, k, v, log_decay, state, lens, scale)

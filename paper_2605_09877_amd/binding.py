@@ -28,6 +28,7 @@ EXPORTS = [
     "kvm_state_export", "kvm_state_import", "kvm_state_profile", "kvm_state_profile_read",
     "kvm_measure_mfma_bf16_peak", "kvm_measure_copy_peak", "kvm_measure_read_peak", "kvm_prepare_scratch_bytes", "kvm_prepare_qkv",
     "kvm_backward_workspace_bytes", "kvm_prefill_backward", "kvm_debug_set",
+    "kvm_linear_workspace_bytes", "kvm_linear_prefill", "kvm_linear_backward", "kvm_linear_decode",
 ]
 (KVM_DEBUG_FOLD_PATH, KVM_DEBUG_FOLD_WAVES, KVM_DEBUG_PREFILL_SCHEDULE, KVM_DEBUG_FOLD_CHAINS, KVM_DEBUG_MERGE_COPY,
  KVM_DEBUG_BACKWARD_PATH, KVM_DEBUG_FOLD_SPLIT, KVM_DEBUG_FOLD_PATIENCE, KVM_DEBUG_COMPUTE_UNITS,
@@ -56,6 +57,11 @@ class kvm_prep_params(C.Structure):
         ("lnq_gamma", C.c_void_p), ("lnq_beta", C.c_void_p), ("lnk_gamma", C.c_void_p), ("lnk_beta", C.c_void_p),
         ("w_gate", C.c_void_p),
     ]
+
+
+class kvm_linear_config(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("io_dtype", C.c_int32), ("scale", C.c_float)]
 
 
 class kvm_grads(C.Structure):
@@ -118,6 +124,12 @@ def load_library() -> C.CDLL:
     lib.kvm_backward_workspace_bytes.restype = C.c_size_t
     lib.kvm_backward_workspace_bytes.argtypes = [vp, i64]
     lib.kvm_prefill_backward.argtypes = [vp] * 10 + [C.POINTER(kvm_grads), i64, vp, C.c_size_t, vp]
+    lin = C.POINTER(kvm_linear_config)
+    lib.kvm_linear_workspace_bytes.restype = C.c_size_t
+    lib.kvm_linear_workspace_bytes.argtypes = [lin, i64]
+    lib.kvm_linear_prefill.argtypes = [lin] + [vp] * 8 + [i64, C.POINTER(kvm_strides), vp, C.c_size_t, vp]
+    lib.kvm_linear_backward.argtypes = [lin] + [vp] * 12 + [i64, vp, C.c_size_t, vp]
+    lib.kvm_linear_decode.argtypes = [lin] + [vp] * 8
     lib.kvm_measure_mfma_bf16_peak.argtypes = [C.c_int, vp, C.POINTER(C.c_double), vp]
     lib.kvm_measure_copy_peak.argtypes = [vp, vp, C.c_size_t, C.POINTER(C.c_double), vp]
     lib.kvm_measure_read_peak.argtypes = [vp, C.c_size_t, vp, C.POINTER(C.c_double), vp]
@@ -587,4 +599,121 @@ def decode_multi_static(states, q, k, v, gate=None, *, out):
         _check(first.lib.kvm_decode_step_multi_static(handles, len(states), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                                       _ptr(gate), out.data_ptr(), _stream()),
                "kvm_decode_step_multi_static")
+    return out
+
+
+# ---- the mixers beside the layer: linear attention with decay
+
+_IO_OF = {torch.bfloat16: KVM_BF16, torch.float32: KVM_F32}
+
+
+def _io_of(q: torch.Tensor) -> int:
+    io = _IO_OF.get(q.dtype)
+    if io is None:
+        raise ValueError(f"q: want torch.bfloat16 or torch.float32, got {q.dtype}")
+    return io
+
+
+def _want(t: Optional[torch.Tensor], shape, dtype, device, name: str, rows: bool = False) -> Optional[int]:
+    """The address of a tensor of that shape, type and device; contiguous, or (rows) with a contiguous last axis.  None: None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or t.device != device or not (
+            (t.stride(-1) == 1 or t.shape[-1] == 1) if rows else t.is_contiguous()):
+        raise ValueError(f"{name}: want {'' if rows else 'contiguous '}{dtype} {tuple(shape)} on {device}"
+                         f"{' with a contiguous last axis' if rows else ''}, got {t.dtype} {tuple(t.shape)} strides {t.stride()} "
+                         f"on {t.device}")
+    return t.data_ptr()
+
+
+def _heads(q: torch.Tensor, k: torch.Tensor):
+    if q.dim() != k.dim() or q.shape[-1] != k.shape[-1] or k.shape[-2] == 0 or q.shape[-2] % k.shape[-2]:
+        raise ValueError(f"q and k: query heads have to be a multiple of KV heads of the same size, got {tuple(q.shape)} and "
+                         f"{tuple(k.shape)}")
+    return q.shape[-2], k.shape[-2], q.shape[-1]
+
+
+def _row_strides(q, k, v, out, lse=None) -> kvm_strides:
+    bth = lambda t: (0, 0, 0) if t is None else (t.stride(0), t.stride(1), t.stride(2))
+    return kvm_strides(*bth(q), *bth(k), *bth(v), *bth(out), 0, 0, 0, *bth(lse))
+
+
+def _linear_config(q, k, scale) -> kvm_linear_config:
+    Hq, Hkv, d = _heads(q, k)
+    return kvm_linear_config(q.shape[0], Hq, Hkv, d, _io_of(q), 0.0 if scale is None else float(scale))
+
+
+def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional[float] = None, out=None, state_out=None):
+    """kvm_linear_prefill: linear attention with a decay for each KV head over T tokens of every sequence.
+    q [B,T,Hq,d]; k, v [B,T,Hkv,d] (bf16 or fp32; views whose head_dim is contiguous); log_decay fp32 [Hkv];
+    state fp32 [B,Hkv,d,d], what a call before has left, or None (zero); lens int32 [B], the sequences' lengths in a padded batch.
+    Returns (out, state_out); state_out may be `state` itself."""
+    lib = load_library()
+    cfg = _linear_config(q, k, scale)
+    B, T = q.shape[:2]
+    dev, Hkv, d = q.device, cfg.n_kv_heads, cfg.head_dim
+    if T == 0:
+        raise ValueError("q: no tokens")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if state_out is None:
+        state_out = torch.empty((B, Hkv, d, d), dtype=torch.float32, device=dev)
+    ptrs = [_want(q, q.shape, q.dtype, dev, "q", True), _want(k, (B, T, Hkv, d), q.dtype, dev, "k", True),
+            _want(v, (B, T, Hkv, d), q.dtype, dev, "v", True), _want(log_decay, (Hkv,), torch.float32, dev, "log_decay"),
+            _want(state, (B, Hkv, d, d), torch.float32, dev, "state"), _want(lens, (B,), torch.int32, dev, "lens"),
+            _want(out, q.shape, q.dtype, dev, "out", True), _want(state_out, (B, Hkv, d, d), torch.float32, dev, "state_out")]
+    nbytes = lib.kvm_linear_workspace_bytes(cfg, T)
+    if nbytes == 0:
+        raise KVMError(KVM_ERR_ARG, "kvm_linear_workspace_bytes: unsupported sizes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    with _on_device(dev):
+        status = lib.kvm_linear_prefill(cfg, *ptrs, T, _row_strides(q, k, v, out), ws.data_ptr(), nbytes, _stream())
+    if status != KVM_OK:
+        _check(status, "kvm_linear_prefill")
+    return out, state_out
+
+
+def linear_backward(q, k, v, log_decay, dout, *, state=None, dstate_out=None, lens=None, scale: Optional[float] = None,
+                    want_dstate: bool = False):
+    """kvm_linear_backward: (dq, dk, dv, dstate or None) of a linear_prefill over these tensors (contiguous)."""
+    lib = load_library()
+    cfg = _linear_config(q, k, scale)
+    B, T = q.shape[:2]
+    dev, Hkv, d = q.device, cfg.n_kv_heads, cfg.head_dim
+    if T == 0:
+        raise ValueError("q: no tokens")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dstate = torch.empty((B, Hkv, d, d), dtype=torch.float32, device=dev) if want_dstate else None
+    ptrs = [_want(q, q.shape, q.dtype, dev, "q"), _want(k, (B, T, Hkv, d), q.dtype, dev, "k"),
+            _want(v, (B, T, Hkv, d), q.dtype, dev, "v"), _want(log_decay, (Hkv,), torch.float32, dev, "log_decay"),
+            _want(state, (B, Hkv, d, d), torch.float32, dev, "state"), _want(lens, (B,), torch.int32, dev, "lens"),
+            _want(dout, q.shape, q.dtype, dev, "dout"), _want(dstate_out, (B, Hkv, d, d), torch.float32, dev, "dstate_out"),
+            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dstate)]
+    nbytes = lib.kvm_linear_workspace_bytes(cfg, T)
+    if nbytes == 0:
+        raise KVMError(KVM_ERR_ARG, "kvm_linear_workspace_bytes: unsupported sizes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    with _on_device(dev):
+        status = lib.kvm_linear_backward(cfg, *ptrs, T, ws.data_ptr(), nbytes, _stream())
+    if status != KVM_OK:
+        _check(status, "kvm_linear_backward")
+    return dq, dk, dv, dstate
+
+
+def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, active=None, out=None):
+    """kvm_linear_decode: one token per sequence; `state` fp32 [B,Hkv,d,d] is advanced in place.  q [B,Hq,d]; k, v [B,Hkv,d];
+    active int32 [B] or None: a sequence whose entry is 0 keeps its state and gets zeros."""
+    lib = load_library()
+    cfg = _linear_config(q, k, scale)
+    B, Hkv, d, dev = q.shape[0], cfg.n_kv_heads, cfg.head_dim, q.device
+    if out is None:
+        out = torch.empty_like(q)
+    ptrs = [_want(state, (B, Hkv, d, d), torch.float32, dev, "state"), _want(q, q.shape, q.dtype, dev, "q"),
+            _want(k, (B, Hkv, d), q.dtype, dev, "k"), _want(v, (B, Hkv, d), q.dtype, dev, "v"),
+            _want(log_decay, (Hkv,), torch.float32, dev, "log_decay"), _want(active, (B,), torch.int32, dev, "active"),
+            _want(out, q.shape, q.dtype, dev, "out")]
+    with _on_device(dev):
+        status = lib.kvm_linear_decode(cfg, *ptrs, _stream())
+    if status != KVM_OK:
+        _check(status, "kvm_linear_decode")
     return out

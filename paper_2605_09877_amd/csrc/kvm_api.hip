@@ -891,6 +891,8 @@ __global__ __launch_bounds__(256) void seqdesc_fill_kernel(StatePack pk, kvm::Se
 
 }  // namespace
 
+int kvm::report_hip(hipError_t e, const char *what) { return hip_fail(e, what); }
+
 extern "C" {
 
 const char *kvm_strerror(int status) {

@@ -15,6 +15,9 @@ inline hipError_t allow_lds(OncePerDevice<hipError_t> &once, const void *kernel,
               [&] { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); });
 }
 
+// kvm_api.hip: keeps the text for kvm_last_hip_error; KVM_ERR_HIP.
+int report_hip(hipError_t e, const char *what);
+
 // A strided source of per-token keys, values and merge gates for all units.
 // Element strides; the head_dim axis is contiguous.  Token index 0 is `k`'s first token.
 struct Src {

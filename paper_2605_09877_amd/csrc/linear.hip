@@ -1,0 +1,598 @@
+// Linear attention with a constant decay for each KV head.
+//
+//   S_t = e^a S_{t-1} + k_t v_t^T,   o_t = scale q_t S_t                       (a <= 0, S fp32 [d, d])
+// A chunk of C tokens with start state S, token i of the chunk:
+//   o_i = scale (sum_{s <= i} e^{a (i - s)} (q_i . k_s) v_s + e^{a (i + 1)} q_i S)
+//   S'  = e^{a C} S + sum_i e^{a (C - 1 - i)} k_i v_i^T
+// Gradients are the same walk in other roles, x the rows asked with, y and z the two factors of the state:
+//   forward  x q   y k   z v    -> out        dq   x dout  y v     z k  (state transposed)
+//   backwards in time, state R = sum over later tokens of e^{a (t - c0 + 1)} q_t dout_t^T (+ the end state's gradient):
+//   dv       x k   y q   z dout               dk   x v     y dout  z q  (state transposed)
+// where x is decayed by e^{a i} and y, z by e^{a (C - i)}, i counted from the chunk's later end (the exponents are one off
+// against the forward walk: kShift).  In the backward walks y and z have the heads of the group, which add up.
+//
+// A workgroup walks one segment of one unit (sequence, KV head); a wave owns 32 channels of z, with S[:, those] in its
+// registers.  S is an operand of x S as it lies there (seq_tiles.h), so it never passes through LDS.
+// Few units: the sequence is cut into segments.  A first pass computes what each adds to the state (y and z alone are
+// read), a second adds those up, and the walk starts every segment from its state.
+#include <math.h>
+
+#include "../../include/kvm.h"
+#include "kvm_internal.h"
+#include "seq_tiles.h"
+
+namespace kvm {
+
+namespace {
+
+struct LinArgs {
+  const char *x, *y, *z;
+  char *out;
+  int64_t x_b, x_t, x_h, y_b, y_t, y_h, z_b, z_t, z_h, o_b, o_t, o_h;   // bytes
+  const float *log_decay;
+  const int32_t *lens;   // nullable
+  const float *start;    // nullable: the state before the first token walked
+  float *seg;            // [units, n_seg, D, D]: start states of the segments (what each adds to the state, after the first pass)
+  float *end;            // nullable: the state behind the last token walked
+  float start_scale, end_scale, scale;
+  int32_t transposed;    // start and seg are [z channel][y channel]
+  int32_t T, H, G, units, n_seg, seg_tokens;
+};
+
+template <typename T>
+constexpr int kChunk = sizeof(T) == 2 ? 64 : 32;   // tokens of a chunk: a tile of either type is C * D * sizeof = 16 KiB at D = 128
+
+template <typename T, int D>
+constexpr size_t linear_lds() {   // two y tiles, z, x, and the powers of the decay
+  return 4 * (size_t)kChunk<T> * D * sizeof(T) + (32 + 2 * kChunk<T>) * sizeof(float);
+}
+
+// kRev: from the last token to the first; kMany: y and z have the heads of the group (otherwise x has); kOut: rows are
+// written, otherwise the state alone is advanced.
+template <typename T, int D, bool kRev, bool kMany, bool kOut>
+__global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int NW = D / 32, C = kChunk<T>, TB = C / 32, KS = D / 16, NB = D / 32, SK = C / 16;
+  constexpr uint32_t kTileB = C * Tl::kRowB;
+  constexpr int kShift = kRev ? 0 : 1;
+  // In bf16 the state enters x S as two operands (16 bits of its significand: its rounding stays below that of the result),
+  // and the decayed z enters the state as three (all 24: the state is an fp32 result).
+  constexpr int kPlanesS = Tl::kBf16 ? 2 : 1, kPlanesZ = Tl::kBf16 ? 3 : 1;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t at_y = lds_addr_of(lds), at_z = at_y + 2 * kTileB, at_x = at_z + kTileB;
+  float *rel = reinterpret_cast<float *>(lds + 4 * kTileB);   // [32 + n]: e^{a n}, n = -32 .. C - 1
+  float *wt = rel + 32 + C;                                   // [i]: the decay of a chunk's token i in the state behind it
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const int u = blockIdx.x % a.units, seg = blockIdx.x / a.units;
+  const int b = u / a.H, h = u % a.H;
+  int n = a.T;
+  if (a.lens) {
+    n = a.lens[b];
+    n = n < 0 ? 0 : n < a.T ? n : a.T;
+  }
+  n = __builtin_amdgcn_readfirstlane(n);
+  const int s0 = seg * a.seg_tokens;
+  const int s1 = s0 + a.seg_tokens < n ? s0 + a.seg_tokens : n;   // positions s0 .. s1 - 1 of the walk
+  const int heads_x = kMany ? 1 : a.G, heads_y = kMany ? a.G : 1;
+  if constexpr (kOut) {   // rows behind the sequence
+    const int z0 = s0 > n ? s0 : n, z1 = s0 + a.seg_tokens < a.T ? s0 + a.seg_tokens : a.T;
+    constexpr int kParts = Tl::kRowB / 16;
+    for (int i = tid; i < (z1 - z0) * heads_x * kParts; i += 64 * NW) {
+      const int part = i % kParts, hx = i / kParts % heads_x, t = z0 + i / (kParts * heads_x);
+      *reinterpret_cast<uint4 *>(a.out + b * a.o_b + (int64_t)t * a.o_t + (int64_t)(h * heads_x + hx) * a.o_h + 16 * part) =
+          make_uint4(0, 0, 0, 0);
+    }
+  }
+  const bool ends = kOut && a.end && (n > 0 ? s0 < n && n <= s0 + a.seg_tokens : seg == 0);
+  if (s0 >= n && !ends) return;
+  if (!kOut && s1 - s0 < a.seg_tokens) return;   // (a segment that another one follows is full)
+
+  // ---- powers of the decay
+  const float al = a.log_decay[h];
+  for (int i = tid; i < 32 + C; i += 64 * NW) rel[i] = i < 32 ? 0.f : expf(al * (float)(i - 32));
+  if (tid < C) wt[tid] = expf(al * (float)(C - kShift - tid));
+  float dec[TB];
+#pragma unroll
+  for (int tb = 0; tb < TB; ++tb) dec[tb] = expf(al * (float)(32 * tb + l32 + kShift)) * a.scale;
+  // e^{a C} as the sum of two floats: hundreds of chunks multiply a slowly decaying state by it, and the rounding
+  // of a single float would be the same one every time
+  double p = exp((double)al * C);
+  float lam_hi = (float)p, lam_lo = (float)(p - (double)lam_hi);
+
+  // ---- the state: element v of block blk is (y channel 32 blk + 16 (v / 8) + 8 g + v % 8, z channel 32 wave + lane % 32)
+  f32x16 S[NB];
+  {
+    const float *src = seg == 0 ? a.start : a.seg + ((int64_t)u * a.n_seg + seg) * (D * D);
+    const float f = seg == 0 ? a.start_scale : 1.f;
+    if (!kOut) src = nullptr;
+    else if (seg == 0 && src) src += (int64_t)u * (D * D);
+    const int zc = 32 * wave + l32;
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int yc = 32 * blk + 16 * (v >> 3) + 8 * g + (v & 7);
+        S[blk][v] = src ? f * src[a.transposed ? zc * D + yc : yc * D + zc] : 0.f;
+      }
+  }
+
+  const char *xb = uniform_ptr(a.x + b * a.x_b + (int64_t)(h * heads_x) * a.x_h);
+  const char *yb = uniform_ptr(a.y + b * a.y_b + (int64_t)(h * heads_y) * a.y_h);
+  const char *zb = uniform_ptr(a.z + b * a.z_b + (int64_t)(h * heads_y) * a.z_h);
+  char *ob = a.out + b * a.o_b + (int64_t)(h * heads_x) * a.o_h;
+  // first row in memory of the chunk at position c0 with nv tokens
+  auto first_row = [&](int c0, int nv) { return kRev ? n - c0 - nv : c0; };
+  auto load_yz = [&](int c0, int hd, uint32_t buf) {
+    const int nv = s1 - c0 < C ? s1 - c0 : C;
+    const int64_t r = first_row(c0, nv);
+    Tl::template fill<C, NW, kRev>(yb + r * a.y_t + hd * a.y_h, (uint32_t)a.y_t, nv, at_y + buf * kTileB, wave, lane);
+    Tl::template fill<C, NW, kRev>(zb + r * a.z_t + hd * a.z_h, (uint32_t)a.z_t, nv, at_z, wave, lane);
+  };
+  auto load_x = [&](int c0, int hd) {
+    const int nv = s1 - c0 < C ? s1 - c0 : C;
+    Tl::template fill<C, NW, kRev>(xb + (int64_t)first_row(c0, nv) * a.x_t + hd * a.x_h, (uint32_t)a.x_t, nv, at_x, wave, lane);
+  };
+
+  Operand<T> xf[TB][KS], zf[SK];
+  f32x16 o[TB];
+  uint32_t buf = 0;
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (s0 < s1) {
+    load_yz(s0, 0, 0);
+    if constexpr (kOut) load_x(s0, 0);
+  }
+  for (int c0 = s0; c0 < s1; c0 += C) {
+    const int nv = s1 - c0 < C ? s1 - c0 : C;
+    for (int hd = 0; hd < a.G; ++hd) {
+      if (!kOut && !kMany && hd > 0) break;
+      const bool new_x = kMany ? hd == 0 : true, new_yz = kMany ? true : hd == 0;
+      const bool last = hd == a.G - 1 || (!kOut && !kMany);
+      const uint32_t y = at_y + buf * kTileB;
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (kOut && new_x) {
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) xf[tb][ks] = Tl::along(at_x, 32 * tb + l32, ks, g);
+      }
+      if (new_yz) {
+#pragma unroll
+        for (int ks = 0; ks < SK; ++ks) zf[ks] = Tl::template across<true>(at_z, wave, ks, lane);
+      }
+      if (nv < C && hd == 0) {   // the last chunk: its tokens decay to the sequence's end
+        if (tid < C) wt[tid] = tid < nv ? expf(al * (float)(nv - kShift - tid)) : 0.f;
+        p = exp((double)al * nv);
+        lam_hi = (float)p;
+        lam_lo = (float)(p - (double)lam_hi);
+      }
+      __builtin_amdgcn_s_waitcnt(0);   // x and z of this step are in registers
+      __syncthreads();
+      {
+        const bool next_chunk = last;
+        const int nc0 = next_chunk ? c0 + C : c0, nhd = next_chunk ? 0 : hd + 1;
+        if (nc0 < s1) {
+          if (kMany || nhd == 0) load_yz(nc0, nhd, buf ^ 1);
+          if (kOut && (!kMany || nhd == 0)) load_x(nc0, nhd);
+        }
+      }
+      if constexpr (kOut) {
+        if (new_x) {   // x S
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[tb][v] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            float s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] = S[ks >> 1][8 * (ks & 1) + e];
+            Operand<T> pl[kPlanesS];
+            split_operand<kPlanesS>(s, pl);
+#pragma unroll
+            for (int i = 0; i < kPlanesS; ++i)
+#pragma unroll
+              for (int tb = 0; tb < TB; ++tb) o[tb] = mma(pl[i], xf[tb][ks], o[tb]);
+          }
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[tb][v] *= dec[tb];
+        }
+        // the chunk's own tokens; the products of a decayed pair enter the second product in the I/O dtype
+#pragma unroll
+        for (int sb = 0; sb < TB; ++sb) {
+          f32x16 sc[TB];
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[tb][v] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const Operand<T> yf = Tl::along(y, 32 * sb + l32, ks, g);
+#pragma unroll
+            for (int tb = sb; tb < TB; ++tb) sc[tb] = mma(yf, xf[tb][ks], sc[tb]);
+          }
+#pragma unroll
+          for (int tb = sb; tb < TB; ++tb)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              float w[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int v = 8 * hf + e, gap = 32 * (tb - sb) + l32 - mfma_row(v, g);
+                w[e] = gap >= 0 ? sc[tb][v] * (rel[32 + gap] * a.scale) : 0.f;
+              }
+              Operand<T> pw;
+              to_operand(w, pw);
+              o[tb] = mma(zf[2 * sb + hf], pw, o[tb]);
+            }
+        }
+        if (kMany ? last : true) {
+          constexpr int es = (int)sizeof(T);
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb) {
+            const int i = 32 * tb + l32;
+            if (i < nv) {
+              const int64_t row = kRev ? n - 1 - (c0 + i) : c0 + i;
+              char *dst = ob + row * a.o_t + (kMany ? 0 : hd * a.o_h) + (32 * wave + 4 * g) * es;
+#pragma unroll
+              for (int vq = 0; vq < 4; ++vq) {
+                if constexpr (Tl::kBf16)
+                  *reinterpret_cast<uint2 *>(dst + 8 * vq * es) =
+                      make_uint2(pack_bf16(o[tb][4 * vq], o[tb][4 * vq + 1]), pack_bf16(o[tb][4 * vq + 2], o[tb][4 * vq + 3]));
+                else
+                  *reinterpret_cast<float4 *>(dst + 8 * vq * es) =
+                      make_float4(o[tb][4 * vq], o[tb][4 * vq + 1], o[tb][4 * vq + 2], o[tb][4 * vq + 3]);
+              }
+            }
+          }
+        }
+      }
+      if (kMany || last) {   // the state behind the chunk
+        if (kMany ? hd == 0 : true) {
+#pragma unroll
+          for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) S[blk][v] = fmaf(S[blk][v], lam_hi, S[blk][v] * lam_lo);
+        }
+#pragma unroll
+        for (int ks = 0; ks < SK; ++ks) {
+          float zs[8];
+          from_operand(zf[ks], zs);
+          const float4 w0 = *reinterpret_cast<const float4 *>(wt + 16 * ks + 4 * g);
+          const float4 w1 = *reinterpret_cast<const float4 *>(wt + 16 * ks + 8 + 4 * g);
+          const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) zs[e] *= w[e];
+          Operand<T> pl[kPlanesZ];
+          split_operand<kPlanesZ>(zs, pl);
+#pragma unroll
+          for (int blk = 0; blk < NB; ++blk) {
+            const Operand<T> yt = Tl::template across<false>(y, blk, ks, lane);
+#pragma unroll
+            for (int i = 0; i < kPlanesZ; ++i) S[blk] = mma(yt, pl[i], S[blk]);
+          }
+        }
+      }
+      if (kMany || last) buf ^= 1;
+    }
+  }
+  float *dst = nullptr;
+  float f = 1.f;
+  if constexpr (kOut) {
+    if (ends) {
+      dst = a.end + (int64_t)u * (D * D);
+      f = a.end_scale;
+    }
+  } else {
+    dst = a.seg + ((int64_t)u * a.n_seg + seg) * (D * D);
+  }
+  if (dst) {
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        dst[(32 * blk + 16 * (v >> 3) + 8 * g + (v & 7)) * D + 32 * wave + l32] = f * S[blk][v];
+  }
+}
+
+// What each segment adds to the state becomes the state it starts from (fp32; as many steps as there are segments).
+__global__ __launch_bounds__(256) void linear_segments_kernel(LinArgs a, int dd) {
+  const int u = blockIdx.y, i = 4 * (blockIdx.x * 256 + threadIdx.x);
+  if (i >= dd) return;
+  int n = a.T;
+  if (a.lens) n = a.lens[u / a.H] < a.T ? a.lens[u / a.H] : a.T;
+  const float lam = (float)exp((double)a.log_decay[u % a.H] * a.seg_tokens);
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (a.start) {
+    s = *reinterpret_cast<const float4 *>(a.start + (int64_t)u * dd + i);
+    s.x *= a.start_scale; s.y *= a.start_scale; s.z *= a.start_scale; s.w *= a.start_scale;
+  }
+  float *at = a.seg + (int64_t)u * a.n_seg * dd + i;
+  for (int seg = 0; seg < a.n_seg; ++seg, at += dd) {
+    if ((int64_t)seg * a.seg_tokens >= n) break;
+    const bool full = (int64_t)(seg + 1) * a.seg_tokens < n;   // another one follows
+    const float4 add = full ? *reinterpret_cast<const float4 *>(at) : make_float4(0.f, 0.f, 0.f, 0.f);
+    *reinterpret_cast<float4 *>(at) = s;
+    s.x = fmaf(s.x, lam, add.x); s.y = fmaf(s.y, lam, add.y); s.z = fmaf(s.z, lam, add.z); s.w = fmaf(s.w, lam, add.w);
+  }
+}
+
+// One token per sequence: the state is read, advanced, written and asked, once.  A workgroup has kCols value channels of one
+// unit; a thread has four of them and D / (256 / (kCols / 4)) key channels.
+struct LinTokenArgs {
+  float *state;
+  const char *q, *k, *v;
+  char *out;
+  const float *log_decay;
+  const int32_t *active;   // nullable
+  float scale;
+  int32_t H, G;
+};
+constexpr int kTokenHeads = 8;   // query heads whose partial sums are in LDS together
+template <typename T, int D, int kCols>
+__global__ __launch_bounds__(256) void linear_token_kernel(LinTokenArgs a) {
+  constexpr int kLanes = kCols / 4, kGroups = 256 / kLanes, kRows = D / kGroups, kParts = D / kCols;
+  __shared__ float qs[kTokenHeads * D], part[kTokenHeads][4][kCols];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int u = blockIdx.x / kParts, col0 = (blockIdx.x % kParts) * kCols;
+  const int b = u / a.H, h = u % a.H, G = a.G;
+  const int c = col0 + 4 * (tid % kLanes), r0 = (tid / kLanes) * kRows;
+  const T *k = (const T *)a.k + (int64_t)u * D, *v = (const T *)a.v + (int64_t)u * D;
+  const T *q = (const T *)a.q + (int64_t)u * G * D;
+  T *out = (T *)a.out + (int64_t)u * G * D;
+  if (a.active && a.active[b] == 0) {
+    for (int i = tid; i < G * kCols; i += 256) Io<T>::store(out + (i / kCols) * D + col0 + i % kCols, 0.f);
+    return;
+  }
+  float *st = a.state + (int64_t)u * (D * D) + (int64_t)r0 * D + c;
+  float4 s[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) s[r] = *reinterpret_cast<const float4 *>(st + r * D);
+  const float lam = expf(a.log_decay[h]);
+  float vv[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) vv[e] = Io<T>::load(v + c + e);
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const float kr = Io<T>::load(k + r0 + r);
+    s[r].x = fmaf(s[r].x, lam, kr * vv[0]);
+    s[r].y = fmaf(s[r].y, lam, kr * vv[1]);
+    s[r].z = fmaf(s[r].z, lam, kr * vv[2]);
+    s[r].w = fmaf(s[r].w, lam, kr * vv[3]);
+    *reinterpret_cast<float4 *>(st + r * D) = s[r];
+  }
+  for (int g0 = 0; g0 < G; g0 += kTokenHeads) {
+    const int ng = G - g0 < kTokenHeads ? G - g0 : kTokenHeads;
+    __syncthreads();
+    for (int i = tid; i < ng * D; i += 256) qs[i] = Io<T>::load(q + g0 * D + i);
+    __syncthreads();
+    for (int hd = 0; hd < ng; ++hd) {
+      float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const float x = qs[hd * D + r0 + r];
+        o[0] = fmaf(x, s[r].x, o[0]);
+        o[1] = fmaf(x, s[r].y, o[1]);
+        o[2] = fmaf(x, s[r].z, o[2]);
+        o[3] = fmaf(x, s[r].w, o[3]);
+      }
+#pragma unroll
+      for (int off = kLanes; off < 64; off *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, kWave);
+      if (lane < kLanes)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[hd][wave][4 * lane + e] = o[e];
+    }
+    __syncthreads();
+    for (int i = tid; i < ng * kCols; i += 256) {
+      const int hd = i / kCols, x = i % kCols;
+      const float o = (part[hd][0][x] + part[hd][1][x]) + (part[hd][2][x] + part[hd][3][x]);
+      Io<T>::store(out + (g0 + hd) * D + col0 + x, o * a.scale);
+    }
+  }
+}
+
+// ---- host side
+
+bool valid(const kvm_linear_config *c) {
+  if (!c || c->batch <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->n_q_heads % c->n_kv_heads) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->io_dtype != KVM_F32 && c->io_dtype != KVM_BF16) return false;
+  if (!(c->scale >= 0.f) || isinf(c->scale)) return false;
+  return (int64_t)c->batch * c->n_q_heads < (1 << 24);
+}
+float scale_of(const kvm_linear_config *c) { return c->scale > 0.f ? c->scale : 1.f / sqrtf((float)c->head_dim); }
+
+// Segments a sequence is cut into: one workgroup has one segment of one unit, and the device holds kFill of them
+// at once.  The first pass reads y and z once more, so a segment has 8 chunks at least.
+struct Cut {
+  int n_seg, seg_tokens;
+};
+Cut cut_of(const kvm_linear_config *c, int64_t T) {
+  const int chunk = c->io_dtype == KVM_BF16 ? kChunk<bf16_t> : kChunk<float>;
+  const int64_t units = (int64_t)c->batch * c->n_kv_heads, chunks = (T + chunk - 1) / chunk;
+  const int64_t fill = c->head_dim == 128 ? 512 : 1024;
+  int64_t n = (fill + units - 1) / units;
+  if (n > chunks / 8) n = chunks / 8;
+  if (n < 1) n = 1;
+  const int64_t per = (chunks + n - 1) / n;
+  return Cut{(int)((chunks + per - 1) / per), (int)(per * chunk)};
+}
+size_t state_bytes(const kvm_linear_config *c) {
+  return (size_t)c->batch * c->n_kv_heads * c->head_dim * c->head_dim * sizeof(float);
+}
+
+template <typename T, int D, bool kRev, bool kMany, bool kOut>
+hipError_t launch_walk_as(const LinArgs &a, int n_wg, hipStream_t st) {
+  static OncePerDevice<hipError_t> once;
+  constexpr size_t bytes = linear_lds<T, D>();
+  hipError_t e = allow_lds(once, (const void *)linear_walk_kernel<T, D, kRev, kMany, kOut>, bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((linear_walk_kernel<T, D, kRev, kMany, kOut>), dim3((unsigned)n_wg), dim3(2 * D), bytes, st, a);
+  return hipGetLastError();
+}
+template <bool kRev, bool kMany, bool kOut>
+hipError_t launch_walk(const kvm_linear_config *c, const LinArgs &a, int n_wg, hipStream_t st) {
+  if (c->io_dtype == KVM_BF16)
+    return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut>(a, n_wg, st)
+                              : launch_walk_as<bf16_t, 64, kRev, kMany, kOut>(a, n_wg, st);
+  return c->head_dim == 128 ? launch_walk_as<float, 128, kRev, kMany, kOut>(a, n_wg, st)
+                            : launch_walk_as<float, 64, kRev, kMany, kOut>(a, n_wg, st);
+}
+hipError_t launch_segments(const kvm_linear_config *c, const LinArgs &a, hipStream_t st) {
+  const int dd = c->head_dim * c->head_dim;
+  hipLaunchKernelGGL(linear_segments_kernel, dim3((unsigned)((dd / 4 + 255) / 256), (unsigned)a.units), dim3(256), 0, st, a, dd);
+  return hipGetLastError();
+}
+
+bool al16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// Strides of one operand, in elements: multiples of 16 bytes, rows whole and apart, 32-bit tile offsets.
+bool strides_ok(int64_t b, int64_t t, int64_t h, const kvm_linear_config *c) {
+  const int vec = c->io_dtype == KVM_BF16 ? 8 : 4;
+  if (b < 0 || t < c->head_dim || h < c->head_dim) return false;
+  if (b % vec || t % vec || h % vec) return false;
+  return t <= (1 << 23);
+}
+
+template <typename T, int D>
+void launch_token_as(const LinTokenArgs &a, int units, hipStream_t st) {
+  if (units < 512)
+    hipLaunchKernelGGL((linear_token_kernel<T, D, 32>), dim3((unsigned)(units * (D / 32))), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((linear_token_kernel<T, D, D>), dim3((unsigned)units), dim3(256), 0, st, a);
+}
+
+}  // namespace
+}  // namespace kvm
+
+extern "C" size_t kvm_linear_workspace_bytes(const kvm_linear_config *cfg, int64_t T) {
+  if (!kvm::valid(cfg) || T <= 0 || T >= (1ll << 31)) return 0;
+  const kvm::Cut cut = kvm::cut_of(cfg, T);
+  return cut.n_seg > 1 ? cut.n_seg * kvm::state_bytes(cfg) : 256;
+}
+
+extern "C" int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, const void *k, const void *v,
+                                  const float *log_decay, const float *state_in, const int32_t *lens, void *out,
+                                  float *state_out, int64_t T, const kvm_strides *strides, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+  using namespace kvm;
+  if (!valid(cfg) || T <= 0 || T >= (1ll << 31) || !q || !k || !v || !log_decay || !out || !workspace) return KVM_ERR_ARG;
+  if (!al16(q) || !al16(k) || !al16(v) || !al16(out) || !al16(state_in) || !al16(state_out) || !al16(workspace)) return KVM_ERR_ARG;
+  if (workspace_bytes < kvm_linear_workspace_bytes(cfg, T)) return KVM_ERR_CAPACITY;
+  const int64_t d = cfg->head_dim, hq = cfg->n_q_heads, hk = cfg->n_kv_heads, es = cfg->io_dtype == KVM_BF16 ? 2 : 4;
+  kvm_strides s;
+  if (strides) s = *strides;
+  else {
+    s.q_b = s.o_b = T * hq * d; s.q_t = s.o_t = hq * d; s.q_h = s.o_h = d;
+    s.k_b = s.v_b = T * hk * d; s.k_t = s.v_t = hk * d; s.k_h = s.v_h = d;
+  }
+  if (!strides_ok(s.q_b, s.q_t, s.q_h, cfg) || !strides_ok(s.k_b, s.k_t, s.k_h, cfg) || !strides_ok(s.v_b, s.v_t, s.v_h, cfg) ||
+      !strides_ok(s.o_b, s.o_t, s.o_h, cfg))
+    return KVM_ERR_ARG;
+  const Cut cut = cut_of(cfg, T);
+  LinArgs a = {};
+  a.x = (const char *)q; a.y = (const char *)k; a.z = (const char *)v; a.out = (char *)out;
+  a.x_b = s.q_b * es; a.x_t = s.q_t * es; a.x_h = s.q_h * es;
+  a.y_b = s.k_b * es; a.y_t = s.k_t * es; a.y_h = s.k_h * es;
+  a.z_b = s.v_b * es; a.z_t = s.v_t * es; a.z_h = s.v_h * es;
+  a.o_b = s.o_b * es; a.o_t = s.o_t * es; a.o_h = s.o_h * es;
+  a.log_decay = log_decay; a.lens = lens; a.start = state_in; a.seg = (float *)workspace; a.end = state_out;
+  a.start_scale = a.end_scale = 1.f; a.scale = scale_of(cfg);
+  a.T = (int32_t)T; a.H = (int32_t)hk; a.G = (int32_t)(hq / hk); a.units = cfg->batch * cfg->n_kv_heads;
+  a.n_seg = cut.n_seg; a.seg_tokens = cut.seg_tokens;
+  hipStream_t st = (hipStream_t)stream;
+  hipError_t e = hipSuccess;
+  if (cut.n_seg > 1) {
+    e = launch_walk<false, false, false>(cfg, a, a.units * (a.n_seg - 1), st);
+    if (e == hipSuccess) e = launch_segments(cfg, a, st);
+  }
+  if (e == hipSuccess) e = launch_walk<false, false, true>(cfg, a, a.units * a.n_seg, st);
+  return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_linear_prefill");
+}
+
+extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, const void *k, const void *v,
+                                   const float *log_decay, const float *state_in, const int32_t *lens, const void *dout,
+                                   const float *dstate_out, void *dq, void *dk, void *dv, float *dstate_in, int64_t T,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
+  using namespace kvm;
+  if (!valid(cfg) || T <= 0 || T >= (1ll << 31) || !q || !k || !v || !log_decay || !dout || !dq || !dk || !dv || !workspace)
+    return KVM_ERR_ARG;
+  const void *ptrs[] = {q, k, v, state_in, dout, dstate_out, dq, dk, dv, dstate_in, workspace};
+  for (const void *x : ptrs)
+    if (!al16(x)) return KVM_ERR_ARG;
+  if (workspace_bytes < kvm_linear_workspace_bytes(cfg, T)) return KVM_ERR_CAPACITY;
+  const int64_t d = cfg->head_dim, hq = cfg->n_q_heads, hk = cfg->n_kv_heads, es = cfg->io_dtype == KVM_BF16 ? 2 : 4;
+  const Cut cut = cut_of(cfg, T);
+  const float scale = scale_of(cfg);
+  hipStream_t st = (hipStream_t)stream;
+  hipError_t e = hipSuccess;
+  if (hq * d > (1 << 23)) return KVM_ERR_ARG;
+  LinArgs c = {};
+  c.log_decay = log_decay; c.lens = lens; c.seg = (float *)workspace; c.scale = scale;
+  c.T = (int32_t)T; c.H = (int32_t)hk; c.G = (int32_t)(hq / hk); c.units = cfg->batch * cfg->n_kv_heads;
+  c.n_seg = cut.n_seg; c.seg_tokens = cut.seg_tokens;
+  auto roles = [&](const void *x, bool xq, const void *y, bool yq, const void *z, bool zq, void *o) {
+    LinArgs a = c;
+    auto put = [&](bool is_q, int64_t &sb, int64_t &s_t, int64_t &sh) {
+      const int64_t hh = is_q ? hq : hk;
+      sb = T * hh * d * es; s_t = hh * d * es; sh = d * es;
+    };
+    a.x = (const char *)x; a.y = (const char *)y; a.z = (const char *)z; a.out = (char *)o;
+    put(xq, a.x_b, a.x_t, a.x_h);
+    put(yq, a.y_b, a.y_t, a.y_h);
+    put(zq, a.z_b, a.z_t, a.z_h);
+    put(xq, a.o_b, a.o_t, a.o_h);
+    return a;
+  };
+  // dq: the forward walk's states, transposed
+  LinArgs f = roles(q, true, k, false, v, false, dq);
+  f.start = state_in; f.start_scale = f.end_scale = 1.f;
+  if (cut.n_seg > 1) {
+    e = launch_walk<false, false, false>(cfg, f, f.units * (f.n_seg - 1), st);
+    if (e == hipSuccess) e = launch_segments(cfg, f, st);
+  }
+  LinArgs a = roles(dout, true, v, false, k, false, dq);
+  a.start = state_in; a.start_scale = 1.f; a.transposed = 1;
+  if (e == hipSuccess) e = launch_walk<false, false, true>(cfg, a, a.units * a.n_seg, st);
+  // dv and dk: backwards; the state there is that of the products q dout, without the scale
+  LinArgs r = roles(k, false, q, true, dout, true, dv);
+  r.start = dstate_out; r.start_scale = 1.f / scale; r.end = dstate_in; r.end_scale = scale;
+  if (cut.n_seg > 1) {
+    if (e == hipSuccess) e = launch_walk<true, true, false>(cfg, r, r.units * (r.n_seg - 1), st);
+    if (e == hipSuccess) e = launch_segments(cfg, r, st);
+  }
+  if (e == hipSuccess) e = launch_walk<true, true, true>(cfg, r, r.units * r.n_seg, st);
+  LinArgs t = roles(v, false, dout, true, q, true, dk);
+  t.start = dstate_out; t.start_scale = 1.f / scale; t.transposed = 1;
+  if (e == hipSuccess) e = launch_walk<true, true, true>(cfg, t, t.units * t.n_seg, st);
+  return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_linear_backward");
+}
+
+extern "C" int kvm_linear_decode(const kvm_linear_config *cfg, float *state, const void *q, const void *k, const void *v,
+                                 const float *log_decay, const int32_t *active, void *out, void *stream) {
+  using namespace kvm;
+  if (!valid(cfg) || !state || !q || !k || !v || !log_decay || !out) return KVM_ERR_ARG;
+  if (!al16(state) || !al16(q) || !al16(k) || !al16(v) || !al16(out)) return KVM_ERR_ARG;
+  LinTokenArgs a;
+  a.state = state; a.q = (const char *)q; a.k = (const char *)k; a.v = (const char *)v; a.out = (char *)out;
+  a.log_decay = log_decay; a.active = active; a.scale = scale_of(cfg);
+  a.H = cfg->n_kv_heads; a.G = cfg->n_q_heads / cfg->n_kv_heads;
+  const int units = cfg->batch * cfg->n_kv_heads;
+  hipStream_t st = (hipStream_t)stream;
+  if (cfg->io_dtype == KVM_BF16) {
+    if (cfg->head_dim == 128) launch_token_as<bf16_t, 128>(a, units, st);
+    else launch_token_as<bf16_t, 64>(a, units, st);
+  } else {
+    if (cfg->head_dim == 128) launch_token_as<float, 128>(a, units, st);
+    else launch_token_as<float, 64>(a, units, st);
+  }
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_linear_decode");
+}

@@ -354,6 +354,51 @@ int kvm_prepare_qkv(const kvm_prep_params *p, const void *q_raw, const void *k_r
                     const void *prev_v, void *q_out, void *k_out, void *v_out, float *gate_out,
                     void *scratch, int64_t T, int64_t pos0, void *stream);
 
+/* ---- Sliding-window attention with sinks --------------------------------------------------------
+ * The other mixer of hybrids: the query at position t sees key j if j <= t and (t - j < window or j < n_sink), in one
+ * softmax of scale * q_t . k_j.  (The KVM layer's own window moves in blocks of C and has no keys that stay.)
+ * Prompts: q, out [B, Tq, H_q, d]; k, v [B, Tk, H_kv, d]; query i stands at position i + Tk - Tq, so that a prompt may be given
+ * in pieces with the keys before it.  lens: nullable device int32 [B], the keys of each sequence of a padded batch (taken as
+ * 0 .. Tk): keys behind are not looked at, queries behind get zeros and lse = -infinity.  In out, values that are not finite
+ * reach the queries that see them and no others; a query all of whose logits are -infinity gets zeros.  In gradients they
+ * also reach keys and queries of the same tiles (up to 128 positions).  Pointers are 16-byte aligned (lse: 4); outputs must not overlap inputs. */
+#define KVM_WINDOW_MAX_SINK 128
+typedef struct kvm_window_config {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim; /* d: 64 or 128; batch * n_q_heads < 2^24 */
+  int32_t io_dtype;                                /* KVM_F32 | KVM_BF16 */
+  int32_t n_sink;                                  /* 0 .. KVM_WINDOW_MAX_SINK */
+  int64_t window;                                  /* keys up to and with the query's own; 1 .. 2^30 - 1 */
+  float scale;                                     /* 0 selects 1 / sqrt(d) */
+} kvm_window_config;
+
+/* Strides as in kvm_prefill_chunked (NULL = dense; gate strides are not looked at), token strides up to 2^23 elements.  lse: [B, Tq, H_q] fp32 natural-log sum of
+ * exponentials, or NULL; out_rest: what rounding out to bf16 left of it, rounded to bf16, in out's shape and strides (for
+ * kvm_window_backward), or NULL; not written with KVM_F32. */
+int kvm_window_prefill(const kvm_window_config *cfg, const void *q, const void *k, const void *v, const int32_t *lens,
+                       void *out, void *out_rest, float *lse, int64_t Tq, int64_t Tk, const kvm_strides *strides,
+                       void *stream);
+
+/* Gradients with respect to q, k and v of that call (all dense): out, out_rest (NULL: D = dout . out is taken over out as
+ * rounded) and lse as it wrote them.  Rows behind a sequence get zero.  workspace: 16-byte aligned, rewritten. */
+size_t kvm_window_backward_workspace_bytes(const kvm_window_config *cfg, int64_t Tq, int64_t Tk);
+int kvm_window_backward(const kvm_window_config *cfg, const void *q, const void *k, const void *v, const int32_t *lens,
+                        const void *out, const void *out_rest, const float *lse, const void *dout, void *dq, void *dk,
+                        void *dv, int64_t Tq, int64_t Tk, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The cache for single tokens: cache_k, cache_v [B, H_kv, n_sink + window, d], the caller's.  Position p is in row p if
+ * p < n_sink, in row n_sink + (p - n_sink) % window otherwise.
+ * kvm_window_fill stores what is left to see of a prompt of T tokens that starts the sequences (k, v strided; lens as
+ * above); rows without a token stay as they were.
+ * kvm_window_decode: one token per sequence at position pos[b] (device int32 [B], >= 0; the tokens before it are in the
+ * cache): stores (k, v) into its row, attends.  pos[b] < 0: no token, nothing is stored and out is zero.
+ *   q, out: [B, H_q, d]; k, v: [B, H_kv, d], dense; workspace: 16-byte aligned, rewritten by every call. */
+int kvm_window_fill(const kvm_window_config *cfg, void *cache_k, void *cache_v, const void *k, const void *v,
+                    const int32_t *lens, int64_t T, const kvm_strides *strides, void *stream);
+size_t kvm_window_decode_workspace_bytes(const kvm_window_config *cfg);
+int kvm_window_decode(const kvm_window_config *cfg, void *cache_k, void *cache_v, const void *q, const void *k,
+                      const void *v, const int32_t *pos, void *out, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
 /* ---- Linear attention with a decay for each KV head ----------------------------------------------
  * A mixer that hybrids put beside the KVM layer, in the same layouts: one fp32 state S [d, d] (key channel, value
  * channel) per sequence and KV head, whatever the tokens seen;

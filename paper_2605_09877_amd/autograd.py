@@ -10,7 +10,8 @@ from typing import Optional
 
 import torch
 
-from .binding import KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, linear_backward, linear_prefill
+from .binding import (KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, linear_backward, linear_prefill, window_backward,
+                      window_prefill)
 
 
 class _KVMAttention(torch.autograd.Function):
@@ -90,3 +91,29 @@ def kvm_linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     if log_decay.requires_grad:
         raise ValueError("log_decay: the decays are constants, they get no gradient")
     return _LinearAttention.apply(q, k, v, log_decay, state, lens, scale)
+
+
+class _WindowAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, window, n_sink, lens, scale):
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        rest = torch.empty_like(q) if q.dtype is torch.bfloat16 else None   # (D = dout . out to 16 bits of out)
+        out, lse = window_prefill(q, k, v, window=window, n_sink=n_sink, lens=lens, scale=scale, want_lse=True, out_rest=rest)
+        ctx.save_for_backward(q, k, v, lens, out, rest, lse)
+        ctx.window, ctx.n_sink, ctx.scale = window, n_sink, scale
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, lens, out, rest, lse = ctx.saved_tensors
+        dq, dk, dv = window_backward(q, k, v, out, lse, dout.contiguous(), window=ctx.window, n_sink=ctx.n_sink, lens=lens,
+                                     scale=ctx.scale, out_rest=rest)
+        return dq, dk, dv, None, None, None, None
+
+
+def kvm_window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, window: int, n_sink: int = 0,
+                         lens: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
+    """Attention over the last `window` keys and the first `n_sink` ones, differentiable in q, k and v.  Shapes and lens as in
+    window_prefill."""
+    return _WindowAttention.apply(q, k, v, window, n_sink, lens, scale)

@@ -19,6 +19,7 @@ KVM_BUDGET_NONE, KVM_BUDGET_FIXED, KVM_BUDGET_SQRT, KVM_BUDGET_TABLE = 0, 1, 2, 
 KVM_OK, KVM_ERR_ARG, KVM_ERR_CAPACITY, KVM_ERR_STATE, KVM_ERR_HIP, KVM_ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 KVM_ERR_LIMIT = -6
 KVM_STATIC_MAX_SEQUENCES = 4096
+KVM_WINDOW_MAX_SINK = 128
 
 EXPORTS = [
     "kvm_strerror", "kvm_last_hip_error", "kvm_state_rows_for", "kvm_state_bytes", "kvm_state_init",
@@ -29,6 +30,8 @@ EXPORTS = [
     "kvm_measure_mfma_bf16_peak", "kvm_measure_copy_peak", "kvm_measure_read_peak", "kvm_prepare_scratch_bytes", "kvm_prepare_qkv",
     "kvm_backward_workspace_bytes", "kvm_prefill_backward", "kvm_debug_set",
     "kvm_linear_workspace_bytes", "kvm_linear_prefill", "kvm_linear_backward", "kvm_linear_decode",
+    "kvm_window_prefill", "kvm_window_backward_workspace_bytes", "kvm_window_backward", "kvm_window_fill",
+    "kvm_window_decode_workspace_bytes", "kvm_window_decode",
 ]
 (KVM_DEBUG_FOLD_PATH, KVM_DEBUG_FOLD_WAVES, KVM_DEBUG_PREFILL_SCHEDULE, KVM_DEBUG_FOLD_CHAINS, KVM_DEBUG_MERGE_COPY,
  KVM_DEBUG_BACKWARD_PATH, KVM_DEBUG_FOLD_SPLIT, KVM_DEBUG_FOLD_PATIENCE, KVM_DEBUG_COMPUTE_UNITS,
@@ -57,6 +60,11 @@ class kvm_prep_params(C.Structure):
         ("lnq_gamma", C.c_void_p), ("lnq_beta", C.c_void_p), ("lnk_gamma", C.c_void_p), ("lnk_beta", C.c_void_p),
         ("w_gate", C.c_void_p),
     ]
+
+
+class kvm_window_config(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("io_dtype", C.c_int32), ("n_sink", C.c_int32), ("window", C.c_int64), ("scale", C.c_float)]
 
 
 class kvm_linear_config(C.Structure):
@@ -130,6 +138,15 @@ def load_library() -> C.CDLL:
     lib.kvm_linear_prefill.argtypes = [lin] + [vp] * 8 + [i64, C.POINTER(kvm_strides), vp, C.c_size_t, vp]
     lib.kvm_linear_backward.argtypes = [lin] + [vp] * 12 + [i64, vp, C.c_size_t, vp]
     lib.kvm_linear_decode.argtypes = [lin] + [vp] * 8
+    win = C.POINTER(kvm_window_config)
+    lib.kvm_window_prefill.argtypes = [win] + [vp] * 7 + [i64, i64, C.POINTER(kvm_strides), vp]
+    lib.kvm_window_backward_workspace_bytes.restype = C.c_size_t
+    lib.kvm_window_backward_workspace_bytes.argtypes = [win, i64, i64]
+    lib.kvm_window_backward.argtypes = [win] + [vp] * 11 + [i64, i64, vp, C.c_size_t, vp]
+    lib.kvm_window_fill.argtypes = [win] + [vp] * 5 + [i64, C.POINTER(kvm_strides), vp]
+    lib.kvm_window_decode_workspace_bytes.restype = C.c_size_t
+    lib.kvm_window_decode_workspace_bytes.argtypes = [win]
+    lib.kvm_window_decode.argtypes = [win] + [vp] * 8 + [C.c_size_t, vp]
     lib.kvm_measure_mfma_bf16_peak.argtypes = [C.c_int, vp, C.POINTER(C.c_double), vp]
     lib.kvm_measure_copy_peak.argtypes = [vp, vp, C.c_size_t, C.POINTER(C.c_double), vp]
     lib.kvm_measure_read_peak.argtypes = [vp, C.c_size_t, vp, C.POINTER(C.c_double), vp]
@@ -602,7 +619,7 @@ def decode_multi_static(states, q, k, v, gate=None, *, out):
     return out
 
 
-# ---- the mixers beside the layer: linear attention with decay
+# ---- the mixers beside the layer: linear attention with decay, sliding-window attention with sinks
 
 _IO_OF = {torch.bfloat16: KVM_BF16, torch.float32: KVM_F32}
 
@@ -627,7 +644,7 @@ def _want(t: Optional[torch.Tensor], shape, dtype, device, name: str, rows: bool
 
 
 def _heads(q: torch.Tensor, k: torch.Tensor):
-    if q.dim() != k.dim() or q.shape[-1] != k.shape[-1] or k.shape[-2] == 0 or q.shape[-2] % k.shape[-2]:
+    if q.dim() < 3 or q.dim() != k.dim() or q.shape[-1] != k.shape[-1] or k.shape[-2] == 0 or q.shape[-2] % k.shape[-2]:
         raise ValueError(f"q and k: query heads have to be a multiple of KV heads of the same size, got {tuple(q.shape)} and "
                          f"{tuple(k.shape)}")
     return q.shape[-2], k.shape[-2], q.shape[-1]
@@ -716,4 +733,109 @@ def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, a
         status = lib.kvm_linear_decode(cfg, *ptrs, _stream())
     if status != KVM_OK:
         _check(status, "kvm_linear_decode")
+    return out
+
+
+def _window_config(B: int, Hq: int, Hkv: int, d: int, io: int, window: int, n_sink: int, scale) -> kvm_window_config:
+    if not 1 <= int(window) < 1 << 30 or not 0 <= int(n_sink) <= KVM_WINDOW_MAX_SINK:
+        raise ValueError(f"window: want 1 .. 2^30 - 1, n_sink 0 .. {KVM_WINDOW_MAX_SINK}, got {window} and {n_sink}")
+    return kvm_window_config(B, Hq, Hkv, d, io, int(n_sink), int(window), 0.0 if scale is None else float(scale))
+
+
+def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: Optional[float] = None, out=None,
+                   want_lse: bool = False, out_rest=None):
+    """kvm_window_prefill: attention over the last `window` keys and the first `n_sink` ones.  q [B,Tq,Hq,d]; k, v [B,Tk,Hkv,d]
+    (bf16 or fp32; views whose head_dim is contiguous), query i at position i + Tk - Tq; lens int32 [B], the sequences' keys in a padded
+    batch.  Returns out, or (out, lse [B,Tq,Hq] fp32)."""
+    lib = load_library()
+    Hq, Hkv, d = _heads(q, k)
+    B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
+    if not 0 < Tq <= Tk:
+        raise ValueError(f"q and k: want 0 < Tq <= Tk, got {Tq} and {Tk}")
+    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    lse = torch.empty((B, Tq, Hq), dtype=torch.float32, device=dev) if want_lse else None
+    if out_rest is not None and out_rest.stride() != out.stride():
+        raise ValueError("out_rest: want the strides of out")
+    ptrs = [_want(q, q.shape, q.dtype, dev, "q", True), _want(k, (B, Tk, Hkv, d), q.dtype, dev, "k", True),
+            _want(v, (B, Tk, Hkv, d), q.dtype, dev, "v", True), _want(lens, (B,), torch.int32, dev, "lens"),
+            _want(out, q.shape, q.dtype, dev, "out", True), _want(out_rest, q.shape, q.dtype, dev, "out_rest", True), _ptr(lse)]
+    with _on_device(dev):
+        status = lib.kvm_window_prefill(cfg, *ptrs, Tq, Tk, _row_strides(q, k, v, out, lse), _stream())
+    if status != KVM_OK:
+        _check(status, "kvm_window_prefill")
+    return (out, lse) if want_lse else out
+
+
+def window_backward(q, k, v, out, lse, dout, *, window: int, n_sink: int = 0, lens=None, scale: Optional[float] = None,
+                    out_rest=None):
+    """kvm_window_backward: (dq, dk, dv) of a window_prefill over these tensors (contiguous)."""
+    lib = load_library()
+    Hq, Hkv, d = _heads(q, k)
+    B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
+    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ptrs = [_want(q, q.shape, q.dtype, dev, "q"), _want(k, (B, Tk, Hkv, d), q.dtype, dev, "k"),
+            _want(v, (B, Tk, Hkv, d), q.dtype, dev, "v"), _want(lens, (B,), torch.int32, dev, "lens"),
+            _want(out, q.shape, q.dtype, dev, "out"), _want(out_rest, q.shape, q.dtype, dev, "out_rest"),
+            _want(lse, (B, Tq, Hq), torch.float32, dev, "lse"), _want(dout, q.shape, q.dtype, dev, "dout"),
+            dq.data_ptr(), dk.data_ptr(), dv.data_ptr()]
+    nbytes = lib.kvm_window_backward_workspace_bytes(cfg, Tq, Tk)
+    if nbytes == 0:
+        raise KVMError(KVM_ERR_ARG, "kvm_window_backward_workspace_bytes: unsupported sizes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    with _on_device(dev):
+        status = lib.kvm_window_backward(cfg, *ptrs, Tq, Tk, ws.data_ptr(), nbytes, _stream())
+    if status != KVM_OK:
+        _check(status, "kvm_window_backward")
+    return dq, dk, dv
+
+
+def window_cache(batch: int, n_kv_heads: int, head_dim: int, *, window: int, n_sink: int = 0, dtype=torch.bfloat16,
+                 device="cuda:0"):
+    """The cache of window_fill and window_decode: (cache_k, cache_v), each [B, Hkv, n_sink + window, d]; contents undefined."""
+    shape = (batch, n_kv_heads, n_sink + window, head_dim)
+    return torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)
+
+
+def window_fill(cache_k, cache_v, k, v, *, window: int, n_sink: int = 0, lens=None) -> None:
+    """kvm_window_fill: what is left to see of a prompt that starts the sequences.  k, v [B,T,Hkv,d]."""
+    lib = load_library()
+    if k.dim() != 4:
+        raise ValueError(f"k: want [B, T, Hkv, d], got {tuple(k.shape)}")
+    B, T, Hkv, d = k.shape
+    dev = k.device
+    cfg = _window_config(B, Hkv, Hkv, d, _io_of(k), window, n_sink, None)
+    rows = (B, Hkv, n_sink + window, d)
+    ptrs = [_want(cache_k, rows, k.dtype, dev, "cache_k"), _want(cache_v, rows, k.dtype, dev, "cache_v"),
+            _want(k, k.shape, k.dtype, dev, "k", True), _want(v, k.shape, k.dtype, dev, "v", True),
+            _want(lens, (B,), torch.int32, dev, "lens")]
+    with _on_device(dev):
+        status = lib.kvm_window_fill(cfg, *ptrs, T, _row_strides(k, k, v, k), _stream())
+    if status != KVM_OK:
+        _check(status, "kvm_window_fill")
+
+
+def window_decode(cache_k, cache_v, q, k, v, pos, *, window: int, n_sink: int = 0, scale: Optional[float] = None, out=None):
+    """kvm_window_decode: one token per sequence, at positions pos (int32 [B]; below 0: no token, zeros), stored into the cache and
+    attended.  q [B,Hq,d]; k, v [B,Hkv,d]."""
+    lib = load_library()
+    Hq, Hkv, d = _heads(q, k)
+    B, dev = q.shape[0], q.device
+    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
+    if out is None:
+        out = torch.empty_like(q)
+    rows = (B, Hkv, n_sink + window, d)
+    ptrs = [_want(cache_k, rows, q.dtype, dev, "cache_k"), _want(cache_v, rows, q.dtype, dev, "cache_v"),
+            _want(q, q.shape, q.dtype, dev, "q"), _want(k, (B, Hkv, d), q.dtype, dev, "k"), _want(v, (B, Hkv, d), q.dtype, dev, "v"),
+            _want(pos, (B,), torch.int32, dev, "pos"), _want(out, q.shape, q.dtype, dev, "out")]
+    nbytes = lib.kvm_window_decode_workspace_bytes(cfg)
+    if nbytes == 0:
+        raise KVMError(KVM_ERR_ARG, "kvm_window_decode_workspace_bytes: unsupported sizes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    with _on_device(dev):
+        status = lib.kvm_window_decode(cfg, *ptrs, ws.data_ptr(), nbytes, _stream())
+    if status != KVM_OK:
+        _check(status, "kvm_window_decode")
     return out

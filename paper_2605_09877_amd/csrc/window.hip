@@ -1,0 +1,1064 @@
+// Sliding-window attention whose first tokens stay visible: the query at position t sees key j if j <= t and
+// (t - j < W or j < S).
+//
+// Prompt: a workgroup's four waves own 32 queries each: of four heads that share a KV head where the group allows it,
+// of consecutive positions otherwise.  Keys come in tiles, the sinks in front of the window first, then the window of
+// the workgroup's first query up to its last query, under one online softmax (seq_tiles.h for the operands):
+//   S^T[key, query] = K Q^T,  P^T = 2^(S^T scale log2 e - m),  O^T[channel, query] += V^T P^T
+#include <math.h>
+
+#include "../../include/kvm.h"
+#include "kvm_internal.h"
+#include "seq_tiles.h"
+
+namespace kvm {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kXcds = 8;
+constexpr int kWaves = 4;
+constexpr int kMaxSink = 128;
+
+struct WinArgs {
+  const char *q, *k, *v;
+  char *out, *rest;   // rest (nullable): what rounding out left, for the backward pass; strides of out
+  float *lse;         // nullable
+  int64_t q_b, q_t, q_h, k_b, k_t, k_h, v_b, v_t, v_h, o_b, o_t, o_h;   // bytes
+  int64_t l_b, l_t, l_h;                                                // elements
+  const int32_t *lens;   // nullable
+  float scale;
+  int32_t B, Hq, Hkv, Tq, Tk, W, S;
+  int32_t by_head, tiles, per_block, blocks;   // position tiles, of which per_block make a block; blocks of a unit
+  // backward
+  const char *dout;
+  char *dq, *dk, *dv;
+  float *delta;    // [B, Hq, Tq]
+  float *part;     // [units, n_split + 1, 2, 128 (S rounded up to 32 used), D]
+  int32_t n_split, split_q;   // ranges that the queries beyond a sink's window are cut into, and their length
+  int32_t key_tiles;
+};
+
+template <typename T, int D>
+constexpr int kTileRows = D * (int)sizeof(T) <= 256 ? 64 : 32;   // keys of a tile: 16 KiB at most
+
+__device__ __forceinline__ int tokens_of(const WinArgs &a, int b) {
+  int n = a.Tk;
+  if (a.lens) {
+    n = a.lens[b];
+    n = n < 0 ? 0 : n < a.Tk ? n : a.Tk;
+  }
+  return __builtin_amdgcn_readfirstlane(n);
+}
+
+// The keys of 32 * kWaves queries at most, first those at positions t0 .. t1 - 1: tiles of the sinks in front of the window, then
+// of the window.
+struct KeyTiles {
+  int lo, n_sink_tiles, n_tiles, sinks, t1;
+  __device__ __forceinline__ KeyTiles(const WinArgs &a, int t0, int t1_, int rows) : t1(t1_) {
+    lo = t0 - a.W + 1 > 0 ? t0 - a.W + 1 : 0;
+    sinks = a.S < lo ? a.S : lo;
+    n_sink_tiles = (sinks + rows - 1) / rows;
+    n_tiles = n_sink_tiles + (t1 - lo + rows - 1) / rows;
+  }
+  __device__ __forceinline__ int first(int it, int rows) const { return it < n_sink_tiles ? it * rows : lo + (it - n_sink_tiles) * rows; }
+  __device__ __forceinline__ int end(int it) const { return it < n_sink_tiles ? sinks : t1; }
+};
+
+// Workgroup -> work item.  Consecutive workgroup ids go round-robin over the 8 XCDs: the workgroups of a block of
+// position tiles of one unit, which read much the same keys, are given to one of them.
+struct Item {
+  int b, hkv, head, tile;   // head: first of the group's that the workgroup has
+  bool none;
+  __device__ __forceinline__ explicit Item(const WinArgs &a) {
+    const int G = a.Hq / a.Hkv, heads = a.by_head ? G / kWaves : G;
+    const int members = a.per_block * heads;
+    const int xcd = blockIdx.x % kXcds, seq = blockIdx.x / kXcds;
+    const int group = seq / members * kXcds + xcd, member = seq % members;
+    const int u = group / a.blocks;
+    tile = group % a.blocks * a.per_block + member / heads;
+    head = member % heads * (a.by_head ? kWaves : 1);
+    b = u / a.Hkv;
+    hkv = u % a.Hkv;
+    none = b >= a.B || tile >= a.tiles;
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void load_row(const char *row, int g, Operand<T> (&f)[D / 16]) {
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) {
+    const uint4 *p = reinterpret_cast<const uint4 *>(row + (16 * ks + 8 * g) * (int)sizeof(T));
+    if constexpr (sizeof(T) == 2) {
+      f[ks].f.q = p[0];
+    } else {
+      float x[4], y[4];
+      unpack16<float>(p[0], x);
+      unpack16<float>(p[1], y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[ks].f[e] = x[e];
+        f[ks].f[4 + e] = y[e];
+      }
+    }
+  }
+}
+
+// Four channels (8 * vq + 4 * g .. + 3 of block blk) of an accumulator's column to memory.
+template <typename T>
+__device__ __forceinline__ void store4(char *row, int blk, int vq, int g, float x, float y, float z, float w) {
+  char *p = row + (32 * blk + 8 * vq + 4 * g) * (int)sizeof(T);
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x, y), pack_bf16(z, w));
+  else *reinterpret_cast<float4 *>(p) = make_float4(x, y, z, w);
+}
+template <typename T>
+__device__ __forceinline__ void load4(const char *row, int blk, int vq, int g, float (&x)[4]) {
+  const char *p = row + (32 * blk + 8 * vq + 4 * g) * (int)sizeof(T);
+  if constexpr (sizeof(T) == 2) {
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    x[0] = __uint_as_float(u.x << 16);
+    x[1] = __uint_as_float(u.x & 0xffff0000u);
+    x[2] = __uint_as_float(u.y << 16);
+    x[3] = __uint_as_float(u.y & 0xffff0000u);
+  } else {
+    const float4 u = *reinterpret_cast<const float4 *>(p);
+    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int KT = kTileRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr uint32_t kTileB = KT * Tl::kRowB;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t at_k = lds_addr_of(lds), at_v = at_k + 2 * kTileB;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const Item w(a);
+  if (w.none) return;
+  const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
+  const int n = tokens_of(a, w.b);
+  const int span = a.by_head ? 32 : 32 * kWaves;
+  const int nq = n - off < 0 ? 0 : n - off;                           // queries of the sequence (n <= Tk: at most Tq)
+  const int Q0 = w.tile * span, Q1 = Q0 + span < nq ? Q0 + span : nq;  // the workgroup's
+  const int hq = w.hkv * G + w.head + (a.by_head ? wave : 0);
+  const int myq = Q0 + (a.by_head ? 0 : 32 * wave) + l32;
+  char *orow = a.out + w.b * a.o_b + (int64_t)myq * a.o_t + (int64_t)hq * a.o_h;
+  float *lse = a.lse ? a.lse + w.b * a.l_b + (int64_t)myq * a.l_t + (int64_t)hq * a.l_h : nullptr;
+  if (myq >= nq && myq < a.Tq) {   // behind the sequence
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) store4<T>(orow, i >> 2, i & 3, g, 0.f, 0.f, 0.f, 0.f);
+    if (lse && g == 0) *lse = -INFINITY;
+  }
+  if (Q0 >= nq) return;
+  const int t = myq + off;   // position of the lane's query
+  const KeyTiles keys(a, Q0 + off, Q1 + off, KT);
+
+  Operand<T> qf[KS];
+  {
+    const int qc = myq < nq ? myq : nq - 1;
+    load_row<T, D>(a.q + w.b * a.q_b + (int64_t)qc * a.q_t + (int64_t)hq * a.q_h, g, qf);
+  }
+  const char *kb = uniform_ptr(a.k + w.b * a.k_b + (int64_t)w.hkv * a.k_h);
+  const char *vb = uniform_ptr(a.v + w.b * a.v_b + (int64_t)w.hkv * a.v_h);
+  auto load_tile = [&](int it) {
+    const int j0 = keys.first(it, KT), nv = keys.end(it) - j0;
+    const uint32_t buf = (uint32_t)(it & 1) * kTileB;
+    Tl::template fill<KT, kWaves, false>(kb + (int64_t)j0 * a.k_t, (uint32_t)a.k_t, nv, at_k + buf, wave, lane);
+    Tl::template fill<KT, kWaves, false>(vb + (int64_t)j0 * a.v_t, (uint32_t)a.v_t, nv, at_v + buf, wave, lane);
+  };
+  const float c = a.scale * kLog2e;
+  f32x16 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const int wt0 = off + Q0 + (a.by_head ? 0 : 32 * wave);   // position of the wave's first query
+  __builtin_amdgcn_s_waitcnt(0);
+  load_tile(0);
+  for (int it = 0; it < keys.n_tiles; ++it) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (it + 1 < keys.n_tiles) load_tile(it + 1);
+    const int j0 = keys.first(it, KT), j1 = keys.end(it);
+    if (j0 > wt0 + 31) continue;   // all behind the wave's queries
+    const uint32_t kt = at_k + (uint32_t)(it & 1) * kTileB, vt = at_v + (uint32_t)(it & 1) * kTileB;
+    f32x16 s[NB];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[blk][v] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) s[blk] = mma(Tl::along(kt, 32 * blk + l32, ks, g), qf[ks], s[blk]);
+    // every pair is visible: keys j0 .. j0 + KT - 1 up to the first query's position and inside the last one's window
+    if (!(j0 + KT <= j1 && j0 + KT - 1 <= wt0 && (wt0 + 31 - j0 < a.W || j0 + KT <= a.S))) {
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int j = j0 + 32 * blk + mfma_row(v, g);
+          const bool sees = j < j1 && j <= t && (t - j < a.W || j < a.S);
+          s[blk][v] = sees ? s[blk][v] : -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, s[blk][v]);
+    top = xhalf_max(top) * c;
+    // m is the reference of the exponentials: it moves when some query's maximum has risen 2^8 above it (in fp32 and bf16 a
+    // p of up to 2^8 is as exact as one of up to 1)
+    const float m_new = fmaxf(m, top);
+    if (__builtin_amdgcn_ballot_w64(m_new > m + 8.f) != 0) {
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[i][v] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen yet)
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[blk][v] = __builtin_amdgcn_exp2f(fmaf(s[blk][v], c, -ref));
+#pragma unroll
+    for (int ks = 0; ks < 2 * NB; ++ks) {
+      // P enters the second product in the I/O dtype; the sum is taken over the rounded values, so that numerator and
+      // denominator see the same ones
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = s[ks >> 1][8 * (ks & 1) + e];
+      Operand<T> pf;
+      to_operand(p, pf);
+      if constexpr (sizeof(T) == 2) {
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pf.f.w[e]), ones, l, false);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) l += p[e];
+      }
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] = mma(Tl::template across<true>(vt, i, ks, lane), pf, o[i]);
+    }
+  }
+  l = xhalf_sum(l);
+  if (myq >= nq) return;
+  // A key that a query does not see enters the second product with p = 0, and a value of it that is not finite makes that NaN: a
+  // query whose result is not finite is done again, one visible key after the other.
+  float bad = 0.f * l;
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bad = fmaf(o[i][v], 0.f, bad);
+  if (!(xhalf_sum(bad) == 0.f)) {
+    const char *qrow = a.q + w.b * a.q_b + (int64_t)myq * a.q_t + (int64_t)hq * a.q_h;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll 1
+    for (int j = 0; j <= t; ++j) {
+      if (j >= a.S && t - j >= a.W) {
+        j = t - a.W;   // (the next one is the window's first)
+        continue;
+      }
+      const char *kr = kb + (int64_t)j * a.k_t, *vr = vb + (int64_t)j * a.v_t;
+      float dot = 0.f;
+#pragma unroll 4
+      for (int i = 0; i < 4 * DB; ++i) {
+        float x[4], y[4];
+        load4<T>(qrow, i >> 2, i & 3, g, x);
+        load4<T>(kr, i >> 2, i & 3, g, y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dot = fmaf(x[e], y[e], dot);
+      }
+      const float x = xhalf_sum(dot) * c, m_new = fmaxf(m, x);
+      if (m_new == -INFINITY) continue;
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(x - m_new);
+      m = m_new;
+      l = fmaf(l, alpha, p);
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+        float y[4];
+        load4<T>(vr, i >> 2, i & 3, g, y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i >> 2][4 * (i & 3) + e] = fmaf(p, y[e], o[i >> 2][4 * (i & 3) + e] * alpha);
+      }
+    }
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // (l = 0: every logit is -infinity)
+#pragma unroll
+  for (int i = 0; i < 4 * DB; ++i) {
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = o[i >> 2][4 * (i & 3) + e] * inv;
+    store4<T>(orow, i >> 2, i & 3, g, x[0], x[1], x[2], x[3]);
+    if constexpr (sizeof(T) == 2) {
+      if (a.rest) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] -= __uint_as_float((uint32_t)float_to_bf16_bits(x[e]) << 16);
+        store4<T>(a.rest + (orow - a.out), i >> 2, i & 3, g, x[0], x[1], x[2], x[3]);
+      }
+    }
+  }
+  if (lse && g == 0) *lse = (m + log2f(l)) * kLn2;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Gradients.  P = 2^(S scale log2 e - lse log2 e) is formed again; D = dout . out of a query, out with what its rounding left;
+//   dS = scale P (dP - D),  dq = dS K (queries stay, keys stream),  dk = dS^T q, dv = P^T dout (keys stay, queries stream).
+// P and dS enter their products in the I/O dtype.
+// (a query all of whose logits are -infinity has nothing of any key: P = 0)
+__device__ __forceinline__ float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_kernel(WinArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int KT = kTileRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr uint32_t kTileB = KT * Tl::kRowB;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t at_k = lds_addr_of(lds), at_v = at_k + 2 * kTileB;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const Item w(a);
+  if (w.none) return;
+  const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
+  const int n = tokens_of(a, w.b);
+  const int span = a.by_head ? 32 : 32 * kWaves;
+  const int nq = n - off < 0 ? 0 : n - off;
+  const int Q0 = w.tile * span, Q1 = Q0 + span < nq ? Q0 + span : nq;
+  const int hq = w.hkv * G + w.head + (a.by_head ? wave : 0);
+  const int myq = Q0 + (a.by_head ? 0 : 32 * wave) + l32;
+  const int64_t at_row = w.b * a.o_b + (int64_t)myq * a.o_t + (int64_t)hq * a.o_h;
+  if (myq >= nq && myq < a.Tq) {
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) store4<T>(a.dq + at_row, i >> 2, i & 3, g, 0.f, 0.f, 0.f, 0.f);
+  }
+  if (Q0 >= nq) return;
+  const int t = myq + off;
+  const KeyTiles keys(a, Q0 + off, Q1 + off, KT);
+  const char *kb = uniform_ptr(a.k + w.b * a.k_b + (int64_t)w.hkv * a.k_h);
+  const char *vb = uniform_ptr(a.v + w.b * a.v_b + (int64_t)w.hkv * a.v_h);
+  auto load_tile = [&](int it) {
+    const int j0 = keys.first(it, KT), nv = keys.end(it) - j0;
+    const uint32_t buf = (uint32_t)(it & 1) * kTileB;
+    Tl::template fill<KT, kWaves, false>(kb + (int64_t)j0 * a.k_t, (uint32_t)a.k_t, nv, at_k + buf, wave, lane);
+    Tl::template fill<KT, kWaves, false>(vb + (int64_t)j0 * a.v_t, (uint32_t)a.v_t, nv, at_v + buf, wave, lane);
+  };
+  load_tile(0);
+  Operand<T> qf[KS], df[KS];
+  float lse2, delta = 0.f;
+  {
+    const int qc = myq < nq ? myq : nq - 1;
+    const int64_t at = w.b * a.o_b + (int64_t)qc * a.o_t + (int64_t)hq * a.o_h;
+    load_row<T, D>(a.q + at, g, qf);
+    load_row<T, D>(a.dout + at, g, df);
+    lse2 = lse_log2(a.lse[w.b * a.l_b + (int64_t)qc * a.l_t + (int64_t)hq * a.l_h]);
+    Operand<T> of[KS];
+    load_row<T, D>(a.out + at, g, of);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      float x[8], y[8];
+      from_operand(of[ks], x);
+      from_operand(df[ks], y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(x[e], y[e], delta);
+    }
+    if constexpr (sizeof(T) == 2) {
+      if (a.rest) {
+        load_row<T, D>(a.rest + at, g, of);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          float x[8], y[8];
+          from_operand(of[ks], x);
+          from_operand(df[ks], y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) delta = fmaf(x[e], y[e], delta);
+        }
+      }
+    }
+    delta = xhalf_sum(delta);
+    if (myq < nq && g == 0) a.delta[((int64_t)w.b * a.Hq + hq) * a.Tq + myq] = delta;
+  }
+  const float c = a.scale * kLog2e;
+  f32x16 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+  const int wt0 = off + Q0 + (a.by_head ? 0 : 32 * wave);
+  __builtin_amdgcn_s_waitcnt(0);
+  for (int it = 0; it < keys.n_tiles; ++it) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (it + 1 < keys.n_tiles) load_tile(it + 1);
+    const int j0 = keys.first(it, KT), j1 = keys.end(it);
+    if (j0 > wt0 + 31) continue;
+    const uint32_t kt = at_k + (uint32_t)(it & 1) * kTileB, vt = at_v + (uint32_t)(it & 1) * kTileB;
+    const bool masked = !(j0 + KT <= j1 && j0 + KT - 1 <= wt0 && (wt0 + 31 - j0 < a.W || j0 + KT <= a.S));
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = dp[v] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mma(Tl::along(kt, 32 * blk + l32, ks, g), qf[ks], s);
+        dp = mma(Tl::along(vt, 32 * blk + l32, ks, g), df[ks], dp);
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        bool sees = true;
+        if (masked) {
+          const int j = j0 + 32 * blk + mfma_row(v, g);
+          sees = j < j1 && j <= t && (t - j < a.W || j < a.S);
+        }
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2));
+        s[v] = sees ? p * (dp[v] - delta) * a.scale : 0.f;
+      }
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[8 * hf + e];
+        Operand<T> ds;
+        to_operand(x, ds);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) o[i] = mma(Tl::template across<true>(kt, i, 2 * blk + hf, lane), ds, o[i]);
+      }
+    }
+  }
+  if (myq >= nq) return;
+#pragma unroll
+  for (int i = 0; i < 4 * DB; ++i)
+    store4<T>(a.dq + at_row, i >> 2, i & 3, g, o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2],
+              o[i >> 2][4 * (i & 3) + 3]);
+}
+
+// dk and dv of 128 keys, 32 to a wave (K in registers, V in LDS); the queries that see them, head after head of the group, stream
+// in tiles of 32.  Sinks (keys below S) are also seen by every query beyond their window: those are cut into n_split ranges with a workgroup
+// each, and what ranges and window give for sinks is added up by window_sinks_kernel.
+template <typename T, int D>
+constexpr size_t kv_lds() {
+  return (4 * 32 + 128) * (size_t)D * sizeof(T) + 2 * 64 * sizeof(float);
+}
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_kernel(WinArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int KS = D / 16, DB = D / 32;
+  constexpr uint32_t kTileB = 32 * Tl::kRowB;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t at_s = lds_addr_of(lds), at_v = at_s + 4 * kTileB;   // stage: q tile, dout tile; then 128 rows of v
+  float *rows = reinterpret_cast<float *>(lds + 8 * kTileB);           // [stage][lse log2 e | D][32]
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq, units = a.B * a.Hkv;
+  const int per_unit = a.key_tiles + a.n_split;
+  // a unit's workgroups go to one XCD
+  const int xcd = blockIdx.x % kXcds, seq = blockIdx.x / kXcds;
+  const int u = seq / per_unit * kXcds + xcd;
+  int member = seq % per_unit;
+  if (u >= units) return;
+  const bool far = member < a.n_split;   // queries beyond the sinks' window (longest: first)
+  const int split = member;
+  if (!far) member -= a.n_split;
+  const int b = u / a.Hkv, hkv = u % a.Hkv;
+  const int n = tokens_of(a, b);
+  const int K0 = far ? 0 : 128 * member;
+  const int kend = far ? (a.S < n ? a.S : n) : (K0 + 128 < n ? K0 + 128 : n);
+  const int key = K0 + 32 * wave + l32;
+  // positions of the queries streamed
+  int t0, t1;
+  if (far) {
+    t0 = a.W + split * a.split_q;
+    t1 = t0 + a.split_q;
+  } else {
+    t0 = K0;
+    t1 = K0 + 127 + a.W;
+  }
+  t0 = t0 > off ? t0 : off;
+  t1 = t1 < n ? t1 : n;
+  const int n_rows = kend > K0 && t1 > t0 ? t1 - t0 : 0;
+  const int n_tiles = (n_rows + 31) / 32 * G;
+
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dk[i][v] = dv[i][v] = 0.f;
+  if (n_tiles > 0) {
+    const char *kb = uniform_ptr(a.k + b * a.k_b + (int64_t)hkv * a.k_h);
+    const char *vb = uniform_ptr(a.v + b * a.v_b + (int64_t)hkv * a.v_h);
+    const char *qb = uniform_ptr(a.q + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
+    const char *db = uniform_ptr(a.dout + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
+    Tl::template fill<128, kWaves, false>(vb + (int64_t)K0 * a.v_t, (uint32_t)a.v_t, kend - K0, at_v, wave, lane);
+    float row = 0.f;
+    auto load_tile = [&](int it) {
+      const int hd = it % G, r0 = it / G * 32, nv = n_rows - r0;
+      const uint32_t at = at_s + (uint32_t)(it & 1) * (2 * kTileB);
+      const int64_t o = (int64_t)r0 * a.o_t + (int64_t)hd * a.o_h;
+      Tl::template fill<32, kWaves, false>(qb + o, (uint32_t)a.o_t, nv, at, wave, lane);
+      Tl::template fill<32, kWaves, false>(db + o, (uint32_t)a.o_t, nv, at + kTileB, wave, lane);
+      if (wave == 0) {   // lse and D of its rows
+        int r = r0 + l32;
+        r = (r < n_rows ? r : n_rows - 1) + t0 - off;
+        row = g == 0 ? lse_log2(a.lse[b * a.l_b + (int64_t)r * a.l_t + (int64_t)(hkv * G + hd) * a.l_h])
+                     : a.delta[((int64_t)b * a.Hq + hkv * G + hd) * a.Tq + r];
+      }
+    };
+    Operand<T> kf[KS];
+    load_tile(0);
+    load_row<T, D>(kb + (int64_t)(key < kend ? key : kend - 1) * a.k_t, g, kf);
+    const float c = a.scale * kLog2e;
+    const int wk0 = K0 + 32 * wave;
+    for (int it = 0; it < n_tiles; ++it) {
+      if (wave == 0) rows[(it & 1) * 64 + lane] = row;
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (it + 1 < n_tiles) load_tile(it + 1);
+      const int p0 = t0 + it / G * 32;   // position of the tile's first query
+      if (wk0 >= kend || (!far && (p0 + 31 < wk0 || p0 - (wk0 + 31) >= a.W))) continue;
+      const uint32_t qt = at_s + (uint32_t)(it & 1) * (2 * kTileB), dt = qt + kTileB;
+      const bool masked = far || !(p0 >= wk0 + 31 && p0 + 31 - wk0 < a.W && p0 + 32 <= t1);
+      f32x16 s, dp;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = dp[v] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s = mma(Tl::along(qt, l32, ks, g), kf[ks], s);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) dp = mma(Tl::along(dt, l32, ks, g), Tl::along(at_v, 32 * wave + l32, ks, g), dp);
+      const float *rl = rows + (it & 1) * 64 + 4 * g;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        float p[8], ds[8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float4 x = *reinterpret_cast<const float4 *>(rl + 16 * hf + 8 * i);
+          const float4 y = *reinterpret_cast<const float4 *>(rl + 32 + 16 * hf + 8 * i);
+          const float lse4[4] = {x.x, x.y, x.z, x.w}, d4[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int v = 8 * hf + 4 * i + e, gap = p0 + mfma_row(v, g) - key;
+            bool sees = true;
+            if (masked)
+              sees = p0 + mfma_row(v, g) < t1 && (far ? key < kend && gap >= a.W : gap >= 0 && gap < a.W);
+            const float pr = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse4[e]));
+            p[4 * i + e] = sees ? pr : 0.f;
+            ds[4 * i + e] = sees ? pr * (dp[v] - d4[e]) * a.scale : 0.f;
+          }
+        }
+        Operand<T> pf, sf;
+        to_operand(p, pf);
+        to_operand(ds, sf);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+          dv[i] = mma(Tl::template across<true>(dt, i, hf, lane), pf, dv[i]);
+          dk[i] = mma(Tl::template across<true>(qt, i, hf, lane), sf, dk[i]);
+        }
+      }
+    }
+  }
+  const int parts = a.n_split + 1;
+  if (far || (a.n_split > 0 && key < a.S)) {   // a sink's share
+    if (key < a.S) {
+      float *pk = a.part + ((((int64_t)u * parts + (far ? split : a.n_split)) * 2) * kMaxSink + key) * D;
+      float *pv = pk + kMaxSink * D;
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int ch = 32 * (i >> 2) + 8 * (i & 3) + 4 * g + e;
+          pk[ch] = dk[i >> 2][4 * (i & 3) + e];
+          pv[ch] = dv[i >> 2][4 * (i & 3) + e];
+        }
+    }
+    return;
+  }
+  if (key < a.Tk) {
+    char *pk = a.dk + b * a.k_b + (int64_t)key * a.k_t + (int64_t)hkv * a.k_h;
+    char *pv = a.dv + b * a.v_b + (int64_t)key * a.v_t + (int64_t)hkv * a.v_h;
+    const float z = key < n ? 1.f : 0.f;   // (a wave's last keys may be behind the sequence)
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      const f32x16 &x = dk[i >> 2], &y = dv[i >> 2];
+      const int v = 4 * (i & 3);
+      if (z != 0.f) {
+        store4<T>(pk, i >> 2, i & 3, g, x[v], x[v + 1], x[v + 2], x[v + 3]);
+        store4<T>(pv, i >> 2, i & 3, g, y[v], y[v + 1], y[v + 2], y[v + 3]);
+      } else {
+        store4<T>(pk, i >> 2, i & 3, g, 0.f, 0.f, 0.f, 0.f);
+        store4<T>(pv, i >> 2, i & 3, g, 0.f, 0.f, 0.f, 0.f);
+      }
+    }
+  }
+}
+
+// dk and dv of the sinks: the sum of their shares, in order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_sinks_kernel(WinArgs a) {
+  const int u = blockIdx.y, b = u / a.Hkv, hkv = u % a.Hkv, parts = a.n_split + 1;
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= 2 * a.S * D) return;
+  const int which = i / (a.S * D), key = i / D % a.S, ch = i % D;
+  if (key >= a.Tk) return;
+  const float *p = a.part + (((int64_t)u * parts * 2 + which) * kMaxSink + key) * D + ch;
+  float sum = 0.f;
+  for (int s = 0; s < parts; ++s) sum += p[(int64_t)s * 2 * kMaxSink * D];
+  if (key >= tokens_of(a, b)) sum = 0.f;
+  char *dst = which ? a.dv + b * a.v_b + (int64_t)key * a.v_t + (int64_t)hkv * a.v_h
+                    : a.dk + b * a.k_b + (int64_t)key * a.k_t + (int64_t)hkv * a.k_h;
+  Io<T>::store((T *)dst + ch, sum);
+}
+
+// ------------------------------------------------------------------------------------------------
+// The ring cache: sinks in rows 0 .. S - 1, position p >= S in row S + (p - S) % W.
+struct CacheArgs {
+  char *ck, *cv;   // [B, Hkv, S + W, D]
+  const char *q, *k, *v;
+  char *out;
+  int64_t k_b, k_t, k_h, v_b, v_t, v_h;   // bytes (fill)
+  const int32_t *at;                       // fill: lens or null; token: positions
+  float *part;                             // [B * Hq, n_split, D + 2]
+  float scale;
+  int64_t W;
+  int32_t B, Hq, Hkv, T, S, n_split, split_rows;
+};
+
+__global__ __launch_bounds__(256) void window_fill_kernel(CacheArgs a, int row_b) {
+  const int64_t rows = a.S + a.W;
+  const int parts = row_b / 16;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * parts) return;
+  const int u = blockIdx.y, b = u / a.Hkv, h = u % a.Hkv, part = (int)(i % parts);
+  const int64_t r = i / parts;
+  int64_t n = a.T;
+  if (a.at) n = a.at[b] < a.T ? a.at[b] : a.T;
+  int64_t p = r;
+  if (r >= a.S && n > a.S) p = r + (n - 1 - r >= 0 ? (n - 1 - r) / a.W * a.W : 0);   // the last position of the row's
+  if (p >= n) return;   // nothing for this row: left as it is
+  const int64_t to = ((int64_t)u * rows + r) * row_b + 16 * part;
+  *reinterpret_cast<uint4 *>(a.ck + to) = *reinterpret_cast<const uint4 *>(a.k + b * a.k_b + p * a.k_t + h * a.k_h + 16 * part);
+  *reinterpret_cast<uint4 *>(a.cv + to) = *reinterpret_cast<const uint4 *>(a.v + b * a.v_b + p * a.v_t + h * a.v_h + 16 * part);
+}
+
+// One token per sequence.  A workgroup has a range of the cache rows of one unit and up to kHeads of its query heads; lanes of a
+// row hold 16 bytes of it each, a wave 1 KiB of consecutive rows at a time.  Every group of lanes keeps a softmax of its
+// own rows; they are joined at the end, those of the ranges by window_join_kernel.
+constexpr int kHeads = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_token_kernel(CacheArgs a) {
+  constexpr int kVec = Vec16<T>::kN, kLanes = D / kVec, kRowsWave = 64 / kLanes, kRowsWg = 4 * kRowsWave;
+  constexpr int kUnroll = 4;
+  __shared__ float part[4][kHeads][D + 2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int G = a.Hq / a.Hkv, batches = (G + kHeads - 1) / kHeads;
+  const int split = blockIdx.x % a.n_split, bu = blockIdx.x / a.n_split;
+  const int u = bu / batches, g0 = bu % batches * kHeads, b = u / a.Hkv;
+  const int ng = G - g0 < kHeads ? G - g0 : kHeads;
+  const int64_t rows = a.S + a.W;
+  const int64_t pos = a.at[b];
+  const int c = lane % kLanes, sub = wave * kRowsWave + lane / kLanes;
+  const int64_t head0 = (int64_t)u * G + g0;   // of [B, Hq]
+  float *po = a.n_split > 1 ? a.part + (head0 * a.n_split + split) * (D + 2) : nullptr;
+  if (pos < 0) {   // no token for this sequence
+    if (split == 0)
+      for (int i = tid; i < ng * D; i += 256) Io<T>::store((T *)a.out + head0 * D + i, 0.f);
+    return;
+  }
+  const int64_t fresh = pos < a.S ? pos : a.S + (pos - a.S) % a.W;   // the token's own row
+  const int64_t r0 = (int64_t)split * a.split_rows;
+  int64_t r1 = r0 + a.split_rows < rows ? r0 + a.split_rows : rows;
+  r1 = r1 <= pos ? r1 : pos + 1;   // rows that hold a token
+  const char *ck = a.ck + (int64_t)u * rows * D * sizeof(T), *cv = a.cv + (int64_t)u * rows * D * sizeof(T);
+  const char *nk = a.k + (int64_t)u * D * sizeof(T), *nv = a.v + (int64_t)u * D * sizeof(T);
+  if (g0 == 0 && fresh >= r0 && fresh < r1 && tid < kLanes) {
+    reinterpret_cast<uint4 *>(a.ck + ((int64_t)u * rows + fresh) * D * sizeof(T))[tid] = reinterpret_cast<const uint4 *>(nk)[tid];
+    reinterpret_cast<uint4 *>(a.cv + ((int64_t)u * rows + fresh) * D * sizeof(T))[tid] = reinterpret_cast<const uint4 *>(nv)[tid];
+  }
+  float q[kHeads][kVec], o[kHeads][kVec], m[kHeads], l[kHeads];
+  const float sc = a.scale * kLog2e;
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) {
+    Vec16<T>::load((const T *)a.q + (head0 + (h < ng ? h : 0)) * D + c * kVec, q[h]);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      q[h][e] *= sc;
+      o[h][e] = 0.f;
+    }
+    m[h] = -INFINITY;
+    l[h] = 0.f;
+  }
+  for (int64_t r = r0 + sub; r < r1; r += kRowsWg * kUnroll) {
+    uint4 kx[kUnroll], vx[kUnroll];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+      int64_t ri = r + i * kRowsWg;
+      ri = ri < r1 ? ri : r;
+      kx[i] = reinterpret_cast<const uint4 *>(ri == fresh ? nk : ck + ri * D * sizeof(T))[c];
+      vx[i] = reinterpret_cast<const uint4 *>(ri == fresh ? nv : cv + ri * D * sizeof(T))[c];
+    }
+    float s[kHeads][kUnroll];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+      float x[kVec];
+      unpack16<T>(kx[i], x);
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        float dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) dot = fmaf(q[h][e], x[e], dot);
+        dot = group_sum<kLanes>(dot);
+        s[h][i] = r + i * kRowsWg < r1 ? dot : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      float top = m[h];
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) top = fmaxf(top, s[h][i]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      const float alpha = __builtin_amdgcn_exp2f(m[h] - ref);
+      m[h] = top;
+      l[h] *= alpha;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) o[h][e] *= alpha;
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) {
+        s[h][i] = __builtin_amdgcn_exp2f(s[h][i] - ref);
+        l[h] += s[h][i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+      if (r + i * kRowsWg < r1) {
+        float x[kVec];
+        unpack16<T>(vx[i], x);
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) o[h][e] = fmaf(s[h][i], x[e], o[h][e]);
+      }
+    }
+  }
+  // join the lane groups of a wave, then the waves
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) {
+    float top = m[h];
+#pragma unroll
+    for (int x = kLanes; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
+    const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[h] - top);
+    l[h] *= f;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) o[h][e] *= f;
+#pragma unroll
+    for (int x = kLanes; x < 64; x *= 2) {
+      l[h] += __shfl_xor(l[h], x, kWave);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) o[h][e] += __shfl_xor(o[h][e], x, kWave);
+    }
+    if (lane < kLanes) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) part[wave][h][c * kVec + e] = o[h][e];
+      if (lane == 0) {
+        part[wave][h][D] = top;
+        part[wave][h][D + 1] = l[h];
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < ng * D; i += 256) {
+    const int h = i / D, ch = i % D;
+    float top = part[0][h][D];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, part[w][h][D]);
+    float sum = 0.f, x = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = part[w][h][D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part[w][h][D] - top);
+      sum = fmaf(f, part[w][h][D + 1], sum);
+      x = fmaf(f, part[w][h][ch], x);
+    }
+    if (po) {
+      float *p = po + (int64_t)h * a.n_split * (D + 2);
+      p[ch] = x;
+      if (ch == 0) {
+        p[D] = top;
+        p[D + 1] = sum;
+      }
+    } else {
+      Io<T>::store((T *)a.out + (head0 + h) * D + ch, sum == 0.f ? 0.f : x / sum);
+    }
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(D) void window_join_kernel(CacheArgs a) {
+  const int64_t head = blockIdx.x;
+  if (a.at[head / a.Hq] < 0) return;
+  const float *p = a.part + head * a.n_split * (D + 2);
+  float top = -INFINITY;
+  for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, p[s * (D + 2) + D]);
+  float sum = 0.f, x = 0.f;
+  for (int s = 0; s < a.n_split; ++s) {
+    const float ms = p[s * (D + 2) + D], f = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - top);
+    if (f != 0.f) {
+      sum = fmaf(f, p[s * (D + 2) + D + 1], sum);
+      x = fmaf(f, p[s * (D + 2) + threadIdx.x], x);
+    }
+  }
+  Io<T>::store((T *)a.out + head * D + threadIdx.x, sum == 0.f ? 0.f : x / sum);
+}
+
+// ---- host side
+
+bool valid(const kvm_window_config *c) {
+  if (!c || c->batch <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->n_q_heads % c->n_kv_heads) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->io_dtype != KVM_F32 && c->io_dtype != KVM_BF16) return false;
+  if (!(c->scale >= 0.f) || isinf(c->scale)) return false;
+  if (c->window < 1 || c->window >= (1ll << 30) || c->n_sink < 0 || c->n_sink > kMaxSink) return false;
+  return (int64_t)c->batch * c->n_q_heads < (1 << 24);
+}
+float scale_of(const kvm_window_config *c) { return c->scale > 0.f ? c->scale : 1.f / sqrtf((float)c->head_dim); }
+bool lengths_ok(int64_t Tq, int64_t Tk) { return Tq > 0 && Tk >= Tq && Tk < (1ll << 30); }
+bool al16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+bool strides_ok(int64_t b, int64_t t, int64_t h, const kvm_window_config *c) {
+  const int vec = c->io_dtype == KVM_BF16 ? 8 : 4;
+  if (b < 0 || t < c->head_dim || h < c->head_dim) return false;
+  if (b % vec || t % vec || h % vec) return false;
+  return t <= (1 << 23);
+}
+
+WinArgs base_args(const kvm_window_config *c, int64_t Tq, int64_t Tk, const int32_t *lens) {
+  WinArgs a = {};
+  a.lens = lens;
+  a.scale = scale_of(c);
+  a.B = c->batch; a.Hq = c->n_q_heads; a.Hkv = c->n_kv_heads;
+  a.Tq = (int32_t)Tq; a.Tk = (int32_t)Tk;
+  a.W = (int32_t)(c->window < Tk ? c->window : Tk);
+  a.S = a.W >= Tk ? 0 : (int32_t)(c->n_sink < Tk ? c->n_sink : Tk);   // (nothing is beyond the window: no sinks needed)
+  const int G = a.Hq / a.Hkv;
+  a.by_head = G % kWaves == 0;
+  a.tiles = (int32_t)((Tq + (a.by_head ? 32 : 128) - 1) / (a.by_head ? 32 : 128));
+  // blocks of position tiles: 2048 positions, fewer where there would not be eight for every XCD
+  int64_t per = a.by_head ? 64 : 16;
+  const int64_t units = (int64_t)a.B * a.Hkv;
+  while (per > 1 && units * ((a.tiles + per - 1) / per) < 8 * kXcds) per /= 2;
+  a.per_block = (int32_t)per;
+  a.blocks = (int32_t)((a.tiles + per - 1) / per);
+  return a;
+}
+// Workgroups of the query kernels, all blocks full and a multiple of eight of them; 0: more than a grid holds.
+unsigned query_grid(const WinArgs &a) {
+  const int64_t G = a.Hq / a.Hkv, groups = ((int64_t)a.B * a.Hkv * a.blocks + kXcds - 1) / kXcds * kXcds;
+  const int64_t n = groups * a.per_block * (a.by_head ? G / kWaves : G);
+  return n < (1ll << 31) ? (unsigned)n : 0;
+}
+// The queries beyond a sink's window: ranges so that the far workgroups stream no more than twice what the others do.
+void cut_far(WinArgs &a) {
+  a.key_tiles = (a.Tk + 127) / 128;
+  if (a.S == 0) return;
+  const int far = a.Tk - a.W;
+  a.split_q = (a.W + 127 + 31) / 32 * 32;
+  if (a.split_q > 1024) a.split_q = 1024;
+  a.n_split = (far + a.split_q - 1) / a.split_q;
+}
+size_t delta_bytes(const WinArgs &a) { return ((size_t)a.B * a.Hq * a.Tq * sizeof(float) + 255) & ~(size_t)255; }
+size_t part_bytes(const WinArgs &a, int d) {
+  return a.n_split ? (size_t)a.B * a.Hkv * (a.n_split + 1) * 2 * kMaxSink * d * sizeof(float) : 0;
+}
+
+template <typename T, int D>
+hipError_t run_prefill(const WinArgs &a, unsigned grid, hipStream_t st) {
+  static OncePerDevice<hipError_t> once;
+  constexpr size_t bytes = 4 * (size_t)kTileRows<T, D> * D * sizeof(T);
+  hipError_t e = allow_lds(once, (const void *)window_prefill_kernel<T, D>, bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((window_prefill_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
+  return hipGetLastError();
+}
+template <typename T, int D>
+hipError_t run_backward_as(const WinArgs &a, unsigned grid, unsigned grid_kv, hipStream_t st) {
+  static OncePerDevice<hipError_t> once_q, once_kv;
+  constexpr size_t bytes = 4 * (size_t)kTileRows<T, D> * D * sizeof(T), bytes_kv = kv_lds<T, D>();
+  hipError_t e = allow_lds(once_q, (const void *)window_dq_kernel<T, D>, bytes);
+  if (e == hipSuccess) e = allow_lds(once_kv, (const void *)window_dkv_kernel<T, D>, bytes_kv);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((window_dkv_kernel<T, D>), dim3(grid_kv), dim3(256), bytes_kv, st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.n_split == 0) return e;
+  hipLaunchKernelGGL((window_sinks_kernel<T, D>), dim3((unsigned)((2 * a.S * D + 255) / 256), (unsigned)(a.B * a.Hkv)), dim3(256), 0,
+                     st, a);
+  return hipGetLastError();
+}
+
+// Ranges a unit's cache rows are cut into: workgroups enough to fill the device, 64 rows at least in each.
+void cut_rows(CacheArgs &a, const kvm_window_config *c) {
+  const int64_t rows = c->n_sink + c->window, G = c->n_q_heads / c->n_kv_heads;
+  const int64_t wgs = (int64_t)c->batch * c->n_kv_heads * ((G + kHeads - 1) / kHeads);
+  int64_t n = (1024 + wgs - 1) / wgs, most = (rows + 63) / 64;
+  if (n > most) n = most;
+  if (n > 64) n = 64;
+  const int64_t per = ((rows + n - 1) / n + 15) / 16 * 16;
+  a.split_rows = (int32_t)per;
+  a.n_split = (int32_t)((rows + per - 1) / per);
+}
+template <typename T, int D>
+hipError_t run_token(const CacheArgs &a, unsigned grid, hipStream_t st) {
+  hipLaunchKernelGGL((window_token_kernel<T, D>), dim3(grid), dim3(256), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.n_split == 1) return e;
+  hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)(a.B * a.Hq)), dim3(D), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace kvm
+
+#define KVM_BY_TYPE(cfg, fn, ...)                                                                    \
+  ((cfg)->io_dtype == KVM_BF16 ? ((cfg)->head_dim == 128 ? fn<bf16_t, 128>(__VA_ARGS__) : fn<bf16_t, 64>(__VA_ARGS__)) \
+                               : ((cfg)->head_dim == 128 ? fn<float, 128>(__VA_ARGS__) : fn<float, 64>(__VA_ARGS__)))
+
+extern "C" int kvm_window_prefill(const kvm_window_config *cfg, const void *q, const void *k, const void *v,
+                                  const int32_t *lens, void *out, void *out_rest, float *lse, int64_t Tq, int64_t Tk,
+                                  const kvm_strides *strides, void *stream) {
+  using namespace kvm;
+  if (!valid(cfg) || !lengths_ok(Tq, Tk) || !q || !k || !v || !out) return KVM_ERR_ARG;
+  if (!al16(q) || !al16(k) || !al16(v) || !al16(out) || !al16(out_rest)) return KVM_ERR_ARG;
+  const int64_t d = cfg->head_dim, hq = cfg->n_q_heads, hk = cfg->n_kv_heads, es = cfg->io_dtype == KVM_BF16 ? 2 : 4;
+  kvm_strides s;
+  if (strides) s = *strides;
+  else {
+    s.q_b = s.o_b = Tq * hq * d; s.q_t = s.o_t = hq * d; s.q_h = s.o_h = d;
+    s.k_b = s.v_b = Tk * hk * d; s.k_t = s.v_t = hk * d; s.k_h = s.v_h = d;
+    s.lse_b = Tq * hq; s.lse_t = hq; s.lse_h = 1;
+  }
+  if (!strides_ok(s.q_b, s.q_t, s.q_h, cfg) || !strides_ok(s.k_b, s.k_t, s.k_h, cfg) || !strides_ok(s.v_b, s.v_t, s.v_h, cfg) ||
+      !strides_ok(s.o_b, s.o_t, s.o_h, cfg))
+    return KVM_ERR_ARG;
+  if (lse && (s.lse_b < 0 || s.lse_t < 1 || s.lse_h < 1)) return KVM_ERR_ARG;
+  WinArgs a = base_args(cfg, Tq, Tk, lens);
+  a.q = (const char *)q; a.k = (const char *)k; a.v = (const char *)v; a.out = (char *)out; a.lse = lse;
+  a.rest = es == 2 ? (char *)out_rest : nullptr;
+  a.q_b = s.q_b * es; a.q_t = s.q_t * es; a.q_h = s.q_h * es;
+  a.k_b = s.k_b * es; a.k_t = s.k_t * es; a.k_h = s.k_h * es;
+  a.v_b = s.v_b * es; a.v_t = s.v_t * es; a.v_h = s.v_h * es;
+  a.o_b = s.o_b * es; a.o_t = s.o_t * es; a.o_h = s.o_h * es;
+  a.l_b = s.lse_b; a.l_t = s.lse_t; a.l_h = s.lse_h;
+  const unsigned grid = query_grid(a);
+  if (grid == 0) return KVM_ERR_ARG;
+  const hipError_t e = KVM_BY_TYPE(cfg, run_prefill, a, grid, (hipStream_t)stream);
+  return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_prefill");
+}
+
+extern "C" size_t kvm_window_backward_workspace_bytes(const kvm_window_config *cfg, int64_t Tq, int64_t Tk) {
+  using namespace kvm;
+  if (!valid(cfg) || !lengths_ok(Tq, Tk)) return 0;
+  WinArgs a = base_args(cfg, Tq, Tk, nullptr);
+  cut_far(a);
+  return delta_bytes(a) + part_bytes(a, cfg->head_dim);
+}
+
+extern "C" int kvm_window_backward(const kvm_window_config *cfg, const void *q, const void *k, const void *v, const int32_t *lens,
+                                   const void *out, const void *out_rest, const float *lse, const void *dout, void *dq,
+                                   void *dk, void *dv, int64_t Tq, int64_t Tk, void *workspace, size_t workspace_bytes,
+                                   void *stream) {
+  using namespace kvm;
+  if (!valid(cfg) || !lengths_ok(Tq, Tk)) return KVM_ERR_ARG;
+  const void *ptrs[] = {q, k, v, out, dout, dq, dk, dv, workspace};
+  for (const void *p : ptrs)
+    if (!p || !al16(p)) return KVM_ERR_ARG;
+  if (!lse || !al16(out_rest)) return KVM_ERR_ARG;
+  const int64_t d = cfg->head_dim, hq = cfg->n_q_heads, hk = cfg->n_kv_heads, es = cfg->io_dtype == KVM_BF16 ? 2 : 4;
+  if (hq * d > (1 << 23)) return KVM_ERR_ARG;
+  if (workspace_bytes < kvm_window_backward_workspace_bytes(cfg, Tq, Tk)) return KVM_ERR_CAPACITY;
+  WinArgs a = base_args(cfg, Tq, Tk, lens);
+  cut_far(a);
+  a.q = (const char *)q; a.k = (const char *)k; a.v = (const char *)v; a.out = (char *)const_cast<void *>(out);
+  a.rest = es == 2 ? (char *)const_cast<void *>(out_rest) : nullptr;
+  a.lse = const_cast<float *>(lse);
+  a.dout = (const char *)dout; a.dq = (char *)dq; a.dk = (char *)dk; a.dv = (char *)dv;
+  a.q_b = a.o_b = Tq * hq * d * es; a.q_t = a.o_t = hq * d * es; a.q_h = a.o_h = d * es;
+  a.k_b = a.v_b = Tk * hk * d * es; a.k_t = a.v_t = hk * d * es; a.k_h = a.v_h = d * es;
+  a.l_b = Tq * hq; a.l_t = hq; a.l_h = 1;
+  a.delta = (float *)workspace;
+  a.part = (float *)((char *)workspace + delta_bytes(a));
+  const unsigned grid = query_grid(a);
+  const int64_t kv = ((int64_t)a.B * a.Hkv + kXcds - 1) / kXcds * kXcds * (a.key_tiles + a.n_split);
+  if (grid == 0 || kv >= (1ll << 31) || (int64_t)a.B * a.Hkv > 65535) return KVM_ERR_ARG;
+  const hipError_t e = KVM_BY_TYPE(cfg, run_backward_as, a, grid, (unsigned)kv, (hipStream_t)stream);
+  return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_backward");
+}
+
+extern "C" int kvm_window_fill(const kvm_window_config *cfg, void *cache_k, void *cache_v, const void *k, const void *v,
+                               const int32_t *lens, int64_t T, const kvm_strides *strides, void *stream) {
+  using namespace kvm;
+  if (!valid(cfg) || !lengths_ok(T, T) || !cache_k || !cache_v || !k || !v) return KVM_ERR_ARG;
+  if (!al16(cache_k) || !al16(cache_v) || !al16(k) || !al16(v)) return KVM_ERR_ARG;
+  const int64_t d = cfg->head_dim, hk = cfg->n_kv_heads, es = cfg->io_dtype == KVM_BF16 ? 2 : 4;
+  kvm_strides s;
+  if (strides) s = *strides;
+  else {
+    s.k_b = s.v_b = T * hk * d; s.k_t = s.v_t = hk * d; s.k_h = s.v_h = d;
+  }
+  if (!strides_ok(s.k_b, s.k_t, s.k_h, cfg) || !strides_ok(s.v_b, s.v_t, s.v_h, cfg)) return KVM_ERR_ARG;
+  const int64_t units = (int64_t)cfg->batch * hk, parts = d * es / 16;
+  if (units > 65535) return KVM_ERR_ARG;
+  CacheArgs a = {};
+  a.ck = (char *)cache_k; a.cv = (char *)cache_v; a.k = (const char *)k; a.v = (const char *)v;
+  a.k_b = s.k_b * es; a.k_t = s.k_t * es; a.k_h = s.k_h * es;
+  a.v_b = s.v_b * es; a.v_t = s.v_t * es; a.v_h = s.v_h * es;
+  a.at = lens; a.W = cfg->window; a.S = cfg->n_sink; a.T = (int32_t)T; a.B = cfg->batch; a.Hkv = (int32_t)hk;
+  const int64_t wgs = ((a.S + a.W) * parts + 255) / 256;
+  if (wgs >= (1ll << 31)) return KVM_ERR_ARG;
+  hipLaunchKernelGGL(window_fill_kernel, dim3((unsigned)wgs, (unsigned)units), dim3(256), 0, (hipStream_t)stream, a, (int)(d * es));
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_fill");
+}
+
+extern "C" size_t kvm_window_decode_workspace_bytes(const kvm_window_config *cfg) {
+  using namespace kvm;
+  if (!valid(cfg)) return 0;
+  CacheArgs a = {};
+  cut_rows(a, cfg);
+  return a.n_split > 1 ? (size_t)cfg->batch * cfg->n_q_heads * a.n_split * (cfg->head_dim + 2) * sizeof(float) : 256;
+}
+
+extern "C" int kvm_window_decode(const kvm_window_config *cfg, void *cache_k, void *cache_v, const void *q, const void *k,
+                                 const void *v, const int32_t *pos, void *out, void *workspace, size_t workspace_bytes,
+                                 void *stream) {
+  using namespace kvm;
+  if (!valid(cfg)) return KVM_ERR_ARG;
+  const void *ptrs[] = {cache_k, cache_v, q, k, v, out, workspace};
+  for (const void *p : ptrs)
+    if (!p || !al16(p)) return KVM_ERR_ARG;
+  if (!pos) return KVM_ERR_ARG;
+  if (workspace_bytes < kvm_window_decode_workspace_bytes(cfg)) return KVM_ERR_CAPACITY;
+  CacheArgs a = {};
+  a.ck = (char *)cache_k; a.cv = (char *)cache_v; a.q = (const char *)q; a.k = (const char *)k; a.v = (const char *)v;
+  a.out = (char *)out; a.at = pos; a.part = (float *)workspace; a.scale = scale_of(cfg);
+  a.W = cfg->window; a.S = cfg->n_sink; a.B = cfg->batch; a.Hq = cfg->n_q_heads; a.Hkv = cfg->n_kv_heads;
+  cut_rows(a, cfg);
+  const int64_t G = a.Hq / a.Hkv, grid = (int64_t)a.B * a.Hkv * ((G + kHeads - 1) / kHeads) * a.n_split;
+  if (grid >= (1ll << 31)) return KVM_ERR_ARG;
+  const hipError_t e = KVM_BY_TYPE(cfg, run_token, a, (unsigned)grid, (hipStream_t)stream);
+  return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_decode");
+}

@@ -127,17 +127,18 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   auto load_yz = [&](int c0, int hd, uint32_t buf) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
     const int64_t r = first_row(c0, nv);
-    Tl::template fill<C, NW, kRev>(yb + r * a.y_t + hd * a.y_h, (uint32_t)a.y_t, nv, at_y + buf * kTileB, wave, lane);
-    Tl::template fill<C, NW, kRev>(zb + r * a.z_t + hd * a.z_h, (uint32_t)a.z_t, nv, at_z, wave, lane);
+    Tl::template fill<C, NW, kRev>(yb + r * a.y_t + hd * a.y_h, (uint32_t)a.y_t, nv, at_y + buf * kTileB, wave, (int)here((uint32_t)lane));
+    Tl::template fill<C, NW, kRev>(zb + r * a.z_t + hd * a.z_h, (uint32_t)a.z_t, nv, at_z, wave, (int)here((uint32_t)lane));
   };
   auto load_x = [&](int c0, int hd) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
-    Tl::template fill<C, NW, kRev>(xb + (int64_t)first_row(c0, nv) * a.x_t + hd * a.x_h, (uint32_t)a.x_t, nv, at_x, wave, lane);
+    Tl::template fill<C, NW, kRev>(xb + (int64_t)first_row(c0, nv) * a.x_t + hd * a.x_h, (uint32_t)a.x_t, nv, at_x, wave, (int)here((uint32_t)lane));
   };
 
   Operand<T> xf[TB][KS], zf[SK];
   f32x16 o[TB];
   uint32_t buf = 0;
+  const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<false>(lane);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if (s0 < s1) {
@@ -150,18 +151,20 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
       if (!kOut && !kMany && hd > 0) break;
       const bool new_x = kMany ? hd == 0 : true, new_yz = kMany ? true : hd == 0;
       const bool last = hd == a.G - 1 || (!kOut && !kMany);
-      const uint32_t y = at_y + buf * kTileB;
+      const uint32_t y_along = here(at_y + buf * kTileB + lane_along), y_across = here(at_y + buf * kTileB + lane_across);
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       if (kOut && new_x) {
+        const uint32_t x = here(at_x + lane_along);
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) xf[tb][ks] = Tl::along(at_x, 32 * tb + l32, ks, g);
+          for (int ks = 0; ks < KS; ++ks) xf[tb][ks] = Tl::along(x, tb, ks);
       }
       if (new_yz) {
+        const uint32_t z = here((at_z + Tl::template across0<true>(lane)) ^ (uint32_t)(32 * wave * (int)sizeof(T)));
 #pragma unroll
-        for (int ks = 0; ks < SK; ++ks) zf[ks] = Tl::template across<true>(at_z, wave, ks, lane);
+        for (int ks = 0; ks < SK; ++ks) zf[ks] = Tl::across(z, 0, ks);
       }
       if (nv < C && hd == 0) {   // the last chunk: its tokens decay to the sequence's end
         if (tid < C) wt[tid] = tid < nv ? expf(al * (float)(nv - kShift - tid)) : 0.f;
@@ -190,6 +193,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
             float s[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[e] = S[ks >> 1][8 * (ks & 1) + e];
+            __builtin_amdgcn_sched_barrier(0);
             Operand<T> pl[kPlanesS];
             split_operand<kPlanesS>(s, pl);
 #pragma unroll
@@ -204,33 +208,30 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
         }
         // the chunk's own tokens; the products of a decayed pair enter the second product in the I/O dtype
 #pragma unroll
-        for (int sb = 0; sb < TB; ++sb) {
-          f32x16 sc[TB];
+        for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-          for (int tb = 0; tb < TB; ++tb)
+          for (int sb = 0; sb <= tb; ++sb) {
+            __builtin_amdgcn_sched_barrier(0);
+            f32x16 sc;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sc[tb][v] = 0.f;
+            for (int v = 0; v < 16; ++v) sc[v] = 0.f;
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            const Operand<T> yf = Tl::along(y, 32 * sb + l32, ks, g);
-#pragma unroll
-            for (int tb = sb; tb < TB; ++tb) sc[tb] = mma(yf, xf[tb][ks], sc[tb]);
-          }
-#pragma unroll
-          for (int tb = sb; tb < TB; ++tb)
+            for (int ks = 0; ks < KS; ++ks) sc = mma(Tl::along(y_along, sb, ks), xf[tb][ks], sc);
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
               float w[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
                 const int v = 8 * hf + e, gap = 32 * (tb - sb) + l32 - mfma_row(v, g);
-                w[e] = gap >= 0 ? sc[tb][v] * (rel[32 + gap] * a.scale) : 0.f;
+                const float r = sc[v] * (rel[32 + gap] * a.scale);
+                w[e] = tb > sb || gap >= 0 ? r : 0.f;
               }
               Operand<T> pw;
               to_operand(w, pw);
               o[tb] = mma(zf[2 * sb + hf], pw, o[tb]);
             }
-        }
+          }
+        __builtin_amdgcn_sched_barrier(0);
         if (kMany ? last : true) {
           constexpr int es = (int)sizeof(T);
 #pragma unroll
@@ -261,6 +262,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
         }
 #pragma unroll
         for (int ks = 0; ks < SK; ++ks) {
+          __builtin_amdgcn_sched_barrier(0);
           float zs[8];
           from_operand(zf[ks], zs);
           const float4 w0 = *reinterpret_cast<const float4 *>(wt + 16 * ks + 4 * g);
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
           split_operand<kPlanesZ>(zs, pl);
 #pragma unroll
           for (int blk = 0; blk < NB; ++blk) {
-            const Operand<T> yt = Tl::template across<false>(y, blk, ks, lane);
+            const Operand<T> yt = Tl::across(y_across, blk, ks);
 #pragma unroll
             for (int i = 0; i < kPlanesZ; ++i) S[blk] = mma(yt, pl[i], S[blk]);
           }

@@ -110,16 +110,21 @@ struct Tile {
     }
   }
 
-  // Operand along a row: tile row `row`, channels 16 * ks + 8 * g .. + 7 (natural order).
-  __device__ static __forceinline__ Operand<T> along(uint32_t at, int row, int ks, int g) {
+  // Operand along a row: tile row 32 * blk + lane % 32, channels 16 * ks + 8 * g .. + 7 (natural order).  base: the tile's LDS
+  // address + along0(lane).  Swizzles repeat every 16 rows and tiles start on 1-KiB borders, so what a step changes of the chunk
+  // is an exclusive or on the address.
+  __device__ static __forceinline__ uint32_t along0(int lane) {
+    const uint32_t l = (uint32_t)lane & 31, g = (uint32_t)lane >> 5;
+    return l * kRowB + 16 * ((kBf16 ? g : 2 * g) ^ swz(l));
+  }
+  __device__ static __forceinline__ Operand<T> along(uint32_t base, int blk, int ks) {
     Operand<T> o;
-    const uint32_t r = at + (uint32_t)row * kRowB, s = swz((uint32_t)row);
     if constexpr (kBf16) {
-      o.f.q = __builtin_bit_cast(uint4, *(const __attribute__((address_space(3))) u32x4_t *)(uintptr_t)(r + 16 * ((uint32_t)(2 * ks + g) ^ s)));
+      o.f.q = __builtin_bit_cast(uint4, *(const __attribute__((address_space(3))) u32x4_t *)(uintptr_t)((base ^ (uint32_t)(32 * ks)) + (uint32_t)(32 * blk * kRowB)));
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const u32x4_t x = *(const __attribute__((address_space(3))) u32x4_t *)(uintptr_t)(r + 16 * ((uint32_t)(4 * ks + 2 * g + i) ^ s));
+        const u32x4_t x = *(const __attribute__((address_space(3))) u32x4_t *)(uintptr_t)((base ^ (uint32_t)(64 * ks + 16 * i)) + (uint32_t)(32 * blk * kRowB));
 #pragma unroll
         for (int e = 0; e < 4; ++e) o.f[4 * i + e] = __uint_as_float(x[e]);
       }
@@ -127,34 +132,45 @@ struct Tile {
     return o;
   }
 
-  // Operand across rows: one channel of block `blk` (32 channels), tile rows row0 + 16 * ks + {4 g + 0..3, 8 + 4 g + 0..3}
-  // (accumulator order).  kNatural: the lane's channel is lane % 32; otherwise the one with which a product's
+  // Operand across rows: one channel of block `blk` (32 channels), tile rows 16 * ks + {4 g + 0..3, 8 + 4 g + 0..3}
+  // (accumulator order).  base: the tile's LDS address + across0.  kNatural: the lane's channel is lane % 32; otherwise the one with which a product's
   // accumulator, its rows being these channels, is in natural order: element v of it is channel 16 * (v / 8) + 8 * g + v % 8.
   template <bool kNatural>
-  __device__ static __forceinline__ Operand<T> across(uint32_t at, int blk, int ks, int lane) {
-    Operand<T> o;
+  __device__ static __forceinline__ uint32_t across0(int lane) {
     const uint32_t g = (uint32_t)lane >> 5;
-    if constexpr (kBf16) {
+    if constexpr (kBf16) {   // the transposing read: lane 4 t + c of 16 addresses row t, piece c of 4 channels
       const uint32_t j = (uint32_t)lane & 15, t = j >> 2, c = j & 3, half = ((uint32_t)lane >> 4) & 1;
-      const uint32_t q = (uint32_t)(4 * blk) + 2 * half + (kNatural ? c >> 1 : c & 1), sub = 8 * (kNatural ? c & 1 : c >> 1);
+      const uint32_t q = 2 * half + (kNatural ? c >> 1 : c & 1), sub = 8 * (kNatural ? c & 1 : c >> 1);
+      return (4 * g + t) * kRowB + 16 * (q ^ swz(4 * g + t)) + sub;
+    } else {
+      const uint32_t l = (uint32_t)lane & 31;
+      const uint32_t ch = kNatural ? l : 16 * (l >> 4) + 8 * ((l >> 2) & 1) + 4 * ((l >> 3) & 1) + (l & 3);
+      return 4 * g * kRowB + 16 * ((ch >> 2) ^ g) + 4 * (ch & 3);
+    }
+  }
+  __device__ static __forceinline__ Operand<T> across(uint32_t base, int blk, int ks) {
+    Operand<T> o;
+    if constexpr (kBf16) {
 #pragma unroll
       for (int hi = 0; hi < 2; ++hi) {
-        const uint32_t r = (uint32_t)(16 * ks + 8 * hi) + 4 * g + t;
-        const uint32_t p = at + r * kRowB + 16 * (q ^ swz(r)) + sub;
+        const uint32_t p = (base ^ (uint32_t)(64 * blk + 32 * hi)) + (uint32_t)((16 * ks + 8 * hi) * kRowB);
         o.f.d[hi] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)(uintptr_t)p));
       }
     } else {
-      const uint32_t l = (uint32_t)lane & 31;
-      const uint32_t ch = (uint32_t)(32 * blk) + (kNatural ? l : 16 * (l >> 4) + 8 * ((l >> 2) & 1) + 4 * ((l >> 3) & 1) + (l & 3));
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t r = (uint32_t)(16 * ks + 8 * (e / 4) + e % 4) + 4 * g;
-        const uint32_t p = at + r * kRowB + 16 * ((ch >> 2) ^ swz(r)) + 4 * (ch & 3);
+        const uint32_t p = (base ^ (uint32_t)((128 * blk) ^ (16 * (4 * (e % 4) + 2 * (e / 4))))) + (uint32_t)((16 * ks + 8 * (e / 4) + e % 4) * kRowB);
         o.f[e] = *(const __attribute__((address_space(3))) float *)(uintptr_t)p;
       }
     }
     return o;
   }
 };
+
+// An address computed where it is used: kept out of registers between uses (loops short of registers).
+__device__ __forceinline__ uint32_t here(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 }  // namespace kvm

@@ -137,6 +137,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
+  const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<true>(lane);
   const Item w(a);
   if (w.none) return;
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int blk = 0; blk < NB; ++blk) s[blk] = mma(Tl::along(kt, 32 * blk + l32, ks, g), qf[ks], s[blk]);
+      for (int blk = 0; blk < NB; ++blk) s[blk] = mma(Tl::along(kt + lane_along, blk, ks), qf[ks], s[blk]);
     // every pair is visible: keys j0 .. j0 + KT - 1 up to the first query's position and inside the last one's window
     if (!(j0 + KT <= j1 && j0 + KT - 1 <= wt0 && (wt0 + 31 - j0 < a.W || j0 + KT <= a.S))) {
 #pragma unroll
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
         for (int e = 0; e < 8; ++e) l += p[e];
       }
 #pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] = mma(Tl::template across<true>(vt, i, ks, lane), pf, o[i]);
+      for (int i = 0; i < DB; ++i) o[i] = mma(Tl::across(vt + lane_across, i, ks), pf, o[i]);
     }
   }
   l = xhalf_sum(l);
@@ -333,6 +334,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
+  const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<true>(lane);
   const Item w(a);
   if (w.none) return;
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
@@ -416,8 +418,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
       for (int v = 0; v < 16; ++v) s[v] = dp[v] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = mma(Tl::along(kt, 32 * blk + l32, ks, g), qf[ks], s);
-        dp = mma(Tl::along(vt, 32 * blk + l32, ks, g), df[ks], dp);
+        s = mma(Tl::along(kt + lane_along, blk, ks), qf[ks], s);
+        dp = mma(Tl::along(vt + lane_along, blk, ks), df[ks], dp);
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -437,7 +439,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
         Operand<T> ds;
         to_operand(x, ds);
 #pragma unroll
-        for (int i = 0; i < DB; ++i) o[i] = mma(Tl::template across<true>(kt, i, 2 * blk + hf, lane), ds, o[i]);
+        for (int i = 0; i < DB; ++i) o[i] = mma(Tl::across(kt + lane_across, i, 2 * blk + hf), ds, o[i]);
       }
     }
   }
@@ -466,6 +468,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
+  const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<true>(lane);
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq, units = a.B * a.Hkv;
   const int per_unit = a.key_tiles + a.n_split;
   // a unit's workgroups go to one XCD
@@ -538,9 +541,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = dp[v] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mma(Tl::along(qt, l32, ks, g), kf[ks], s);
+      for (int ks = 0; ks < KS; ++ks) s = mma(Tl::along(qt + lane_along, 0, ks), kf[ks], s);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) dp = mma(Tl::along(dt, l32, ks, g), Tl::along(at_v, 32 * wave + l32, ks, g), dp);
+      for (int ks = 0; ks < KS; ++ks) dp = mma(Tl::along(dt + lane_along, 0, ks), Tl::along(at_v + (uint32_t)(32 * wave * Tl::kRowB) + lane_along, 0, ks), dp);
       const float *rl = rows + (it & 1) * 64 + 4 * g;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
@@ -566,8 +569,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
         to_operand(ds, sf);
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
-          dv[i] = mma(Tl::template across<true>(dt, i, hf, lane), pf, dv[i]);
-          dk[i] = mma(Tl::template across<true>(qt, i, hf, lane), sf, dk[i]);
+          dv[i] = mma(Tl::across(dt + lane_across, i, hf), pf, dv[i]);
+          dk[i] = mma(Tl::across(qt + lane_across, i, hf), sf, dk[i]);
         }
       }
     }

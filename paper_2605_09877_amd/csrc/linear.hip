@@ -17,6 +17,8 @@
 // read), a second adds those up, and the walk starts every segment from its state.
 #include <math.h>
 
+#include <type_traits>
+
 #include "../../include/kvm.h"
 #include "kvm_internal.h"
 #include "seq_tiles.h"
@@ -36,35 +38,48 @@ struct LinArgs {
   float *end;            // nullable: the state behind the last token walked
   float start_scale, end_scale, scale;
   int32_t transposed;    // start and seg are [z channel][y channel]
+  int32_t fine_state;    // the state is a result
   int32_t T, H, G, units, n_seg, seg_tokens;
 };
 
 template <typename T>
 constexpr int kChunk = sizeof(T) == 2 ? 64 : 32;   // tokens of a chunk: a tile of either type is C * D * sizeof = 16 KiB at D = 128
 
-template <typename T, int D>
-constexpr size_t linear_lds() {   // two y tiles, z, x, and the powers of the decay
-  return 4 * (size_t)kChunk<T> * D * sizeof(T) + (32 + 2 * kChunk<T>) * sizeof(float);
+// Blocks of 32 x 32 pairs of a chunk, row block tb and column block sb <= tb: 0: (0, 0), 1: (1, 0), 2: (1, 1).
+template <typename T>
+constexpr int kBlocks = kChunk<T> == 64 ? 3 : 1;
+
+// Two y tiles, z, x; pairs of a chunk as operands (bf16); the powers of the decay.
+template <typename T, int D, bool kFine>
+constexpr size_t linear_lds() {
+  return 4 * (size_t)kChunk<T> * D * sizeof(T) + (sizeof(T) == 2 ? kBlocks<T> * (kFine ? 4096 : 2048) : 0) +
+         (32 + 2 * kChunk<T>) * sizeof(float);
 }
 
 // kRev: from the last token to the first; kMany: y and z have the heads of the group (otherwise x has); kOut: rows are
 // written, otherwise the state alone is advanced.
-template <typename T, int D, bool kRev, bool kMany, bool kOut>
+// Roundings in bf16 (sums and states are fp32 throughout): the state enters x S, and the decayed pairs of a chunk the product
+// with z, as one operand each, which leaves an output twice the variance of its own rounding; kFine: as two, with
+// errors of 2^-16, for prompts so short that an output rests on a few pairs.  The decayed z enters the state as three
+// operands, all 24 bits, where the state is a result, as two elsewhere (a.fine_state).
+template <typename T, int D, bool kRev, bool kMany, bool kOut, bool kFine>
 __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   using Tl = Tile<T, D>;
   constexpr int NW = D / 32, C = kChunk<T>, TB = C / 32, KS = D / 16, NB = D / 32, SK = C / 16;
   constexpr uint32_t kTileB = C * Tl::kRowB;
   constexpr int kShift = kRev ? 0 : 1;
-  // In bf16 the state enters x S as two operands (16 bits of its significand: its rounding stays below that of the result),
-  // and the decayed z enters the state as three (all 24: the state is an fp32 result).
-  constexpr int kPlanesS = Tl::kBf16 ? 2 : 1, kPlanesZ = Tl::kBf16 ? 3 : 1;
+  constexpr int kPlanes = Tl::kBf16 && kFine ? 2 : 1, kPlanesZ = Tl::kBf16 ? 3 : 1;
+  constexpr bool kShare = Tl::kBf16;   // each pair block by one wave, passed on through LDS (fp32 has one block: every wave makes it)
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t at_y = lds_addr_of(lds), at_z = at_y + 2 * kTileB, at_x = at_z + kTileB;
-  float *rel = reinterpret_cast<float *>(lds + 4 * kTileB);   // [32 + n]: e^{a n}, n = -32 .. C - 1
-  float *wt = rel + 32 + C;                                   // [i]: the decay of a chunk's token i in the state behind it
+  char *pairs = lds + 4 * kTileB;
+  float *rel = reinterpret_cast<float *>(pairs + (kShare ? kBlocks<T> * kPlanes * 2048 : 0));   // [32 + n]: scale e^{a n}, n = -32 .. C - 1
+  float *wt = rel + 32 + C;   // [i]: the decay of a chunk's token i in the state behind it
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
+  // the lane's z channel of its wave's 32: such that results, which have z channels as rows, are in natural order
+  const int zl = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
   const int u = blockIdx.x % a.units, seg = blockIdx.x / a.units;
   const int b = u / a.H, h = u % a.H;
   int n = a.T;
@@ -91,24 +106,25 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
 
   // ---- powers of the decay
   const float al = a.log_decay[h];
-  for (int i = tid; i < 32 + C; i += 64 * NW) rel[i] = i < 32 ? 0.f : expf(al * (float)(i - 32));
+  for (int i = tid; i < 32 + C; i += 64 * NW) rel[i] = i < 32 ? 0.f : a.scale * expf(al * (float)(i - 32));
   if (tid < C) wt[tid] = expf(al * (float)(C - kShift - tid));
   float dec[TB];
 #pragma unroll
   for (int tb = 0; tb < TB; ++tb) dec[tb] = expf(al * (float)(32 * tb + l32 + kShift)) * a.scale;
-  // e^{a C} as the sum of two floats: hundreds of chunks multiply a slowly decaying state by it, and the rounding
-  // of a single float would be the same one every time
-  double p = exp((double)al * C);
-  float lam_hi = (float)p, lam_lo = (float)(p - (double)lam_hi);
+  // e^{a C} as a float, and what that leaves.  Hundreds of chunks multiply a slowly decaying state by it, and the rounding of a
+  // single float would be the same one every time: the rest is carried from chunk to chunk.
+  const double lam = exp((double)al * C);
+  const float lam_hi = (float)lam, lam_lo = (float)(lam - (double)lam_hi);
+  float carry = 0.f;
 
-  // ---- the state: element v of block blk is (y channel 32 blk + 16 (v / 8) + 8 g + v % 8, z channel 32 wave + lane % 32)
+  // ---- the state: element v of block blk is (y channel 32 blk + 16 (v / 8) + 8 g + v % 8, z channel 32 wave + zl)
   f32x16 S[NB];
   {
     const float *src = seg == 0 ? a.start : a.seg + ((int64_t)u * a.n_seg + seg) * (D * D);
     const float f = seg == 0 ? a.start_scale : 1.f;
     if (!kOut) src = nullptr;
     else if (seg == 0 && src) src += (int64_t)u * (D * D);
-    const int zc = 32 * wave + l32;
+    const int zc = 32 * wave + zl;
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
@@ -127,18 +143,41 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   auto load_yz = [&](int c0, int hd, uint32_t buf) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
     const int64_t r = first_row(c0, nv);
-    Tl::template fill<C, NW, kRev>(yb + r * a.y_t + hd * a.y_h, (uint32_t)a.y_t, nv, at_y + buf * kTileB, wave, (int)here((uint32_t)lane));
-    Tl::template fill<C, NW, kRev>(zb + r * a.z_t + hd * a.z_h, (uint32_t)a.z_t, nv, at_z, wave, (int)here((uint32_t)lane));
+    const int ln = (int)here((uint32_t)lane);
+    Tl::template fill<C, NW, kRev>(yb + r * a.y_t + hd * a.y_h, (uint32_t)a.y_t, nv, at_y + buf * kTileB, wave, ln);
+    Tl::template fill<C, NW, kRev>(zb + r * a.z_t + hd * a.z_h, (uint32_t)a.z_t, nv, at_z, wave, ln);
   };
   auto load_x = [&](int c0, int hd) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
-    Tl::template fill<C, NW, kRev>(xb + (int64_t)first_row(c0, nv) * a.x_t + hd * a.x_h, (uint32_t)a.x_t, nv, at_x, wave, (int)here((uint32_t)lane));
+    Tl::template fill<C, NW, kRev>(xb + (int64_t)first_row(c0, nv) * a.x_t + hd * a.x_h, (uint32_t)a.x_t, nv, at_x, wave,
+                                   (int)here((uint32_t)lane));
   };
 
   Operand<T> xf[TB][KS], zf[SK];
   f32x16 o[TB];
   uint32_t buf = 0;
+  bool stored = false;   // full rows have been stored behind the latest loads
   const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<false>(lane);
+  // the decayed pairs of block (tb, sb) as operands of the second product: z^T . pairs
+  auto pairs_of = [&](auto tb_, auto sb_, uint32_t y_along, Operand<T> (&pw)[2][kPlanes]) {
+    constexpr int tb = decltype(tb_)::value, sb = decltype(sb_)::value;
+    f32x16 sc = {0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) sc = mma(Tl::along(y_along, sb, ks), xf[tb][ks], sc);
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int v = 8 * hf + e, gap = 32 * (tb - sb) + l32 - mfma_row(v, g);
+        const float r = sc[v] * rel[32 + gap];
+        w[e] = tb > sb || gap >= 0 ? r : 0.f;
+      }
+      split_operand<kPlanes>(w, pw[hf]);
+    }
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, TB - 1>;
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if (s0 < s1) {
@@ -152,8 +191,13 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
       const bool new_x = kMany ? hd == 0 : true, new_yz = kMany ? true : hd == 0;
       const bool last = hd == a.G - 1 || (!kOut && !kMany);
       const uint32_t y_along = here(at_y + buf * kTileB + lane_along), y_across = here(at_y + buf * kTileB + lane_across);
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
+      // this step's tiles: asked for ahead of the stores of the step before, which need not have ended (a lane stores
+      // kStores times for a full chunk)
+      constexpr int kStores = TB * 32 * (int)sizeof(T) / 32;
+      if (stored) wait_vmem<kStores>();
+      else wait_vmem<0>();
+      publish();
+      stored = false;
       if (kOut && new_x) {
         const uint32_t x = here(at_x + lane_along);
 #pragma unroll
@@ -162,21 +206,28 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
           for (int ks = 0; ks < KS; ++ks) xf[tb][ks] = Tl::along(x, tb, ks);
       }
       if (new_yz) {
-        const uint32_t z = here((at_z + Tl::template across0<true>(lane)) ^ (uint32_t)(32 * wave * (int)sizeof(T)));
+        const uint32_t z = here((at_z + lane_across) ^ (uint32_t)(32 * wave * (int)sizeof(T)));
 #pragma unroll
         for (int ks = 0; ks < SK; ++ks) zf[ks] = Tl::across(z, 0, ks);
       }
-      if (nv < C && hd == 0) {   // the last chunk: its tokens decay to the sequence's end
-        if (tid < C) wt[tid] = tid < nv ? expf(al * (float)(nv - kShift - tid)) : 0.f;
-        p = exp((double)al * nv);
-        lam_hi = (float)p;
-        lam_lo = (float)(p - (double)lam_hi);
+      if (nv < C && hd == 0 && tid < C) wt[tid] = tid < nv ? expf(al * (float)(nv - kShift - tid)) : 0.f;   // (decay to the end)
+      if constexpr (kOut && kShare) {
+        auto pass_on = [&](int i, auto tb, auto sb) {
+          Operand<T> pw[2][kPlanes];
+          pairs_of(tb, sb, y_along, pw);
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int pl = 0; pl < kPlanes; ++pl)
+              *reinterpret_cast<Operand<T> *>(pairs + ((2 * i + hf) * kPlanes + pl) * 1024 + 16 * lane) = pw[hf][pl];
+        };
+        if (wave == 1) pass_on(0, I0{}, I0{});
+        if (wave == 0) pass_on(1, I1{}, I0{});
+        if (wave == (NW > 2 ? 2 : 1)) pass_on(2, I1{}, I1{});
       }
-      __builtin_amdgcn_s_waitcnt(0);   // x and z of this step are in registers
-      __syncthreads();
+      publish();   // x and z of this step are in registers, its pairs in LDS
       {
-        const bool next_chunk = last;
-        const int nc0 = next_chunk ? c0 + C : c0, nhd = next_chunk ? 0 : hd + 1;
+        const int nc0 = last ? c0 + C : c0, nhd = last ? 0 : hd + 1;
         if (nc0 < s1) {
           if (kMany || nhd == 0) load_yz(nc0, nhd, buf ^ 1);
           if (kOut && (!kMany || nhd == 0)) load_x(nc0, nhd);
@@ -185,19 +236,16 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
       if constexpr (kOut) {
         if (new_x) {   // x S
 #pragma unroll
-          for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[tb][v] = 0.f;
+          for (int tb = 0; tb < TB; ++tb) o[tb] = f32x16{0.f};
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
             float s[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[e] = S[ks >> 1][8 * (ks & 1) + e];
-            __builtin_amdgcn_sched_barrier(0);
-            Operand<T> pl[kPlanesS];
-            split_operand<kPlanesS>(s, pl);
+            Operand<T> pl[kPlanes];
+            split_operand<kPlanes>(s, pl);
 #pragma unroll
-            for (int i = 0; i < kPlanesS; ++i)
+            for (int i = 0; i < kPlanes; ++i)
 #pragma unroll
               for (int tb = 0; tb < TB; ++tb) o[tb] = mma(pl[i], xf[tb][ks], o[tb]);
           }
@@ -206,48 +254,41 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[tb][v] *= dec[tb];
         }
-        // the chunk's own tokens; the products of a decayed pair enter the second product in the I/O dtype
+        // the chunk's own tokens
+        if constexpr (kShare) {
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb)
+          for (int i = 0; i < kBlocks<T>; ++i)
 #pragma unroll
-          for (int sb = 0; sb <= tb; ++sb) {
-            __builtin_amdgcn_sched_barrier(0);
-            f32x16 sc;
+            for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sc[v] = 0.f;
+              for (int pl = 0; pl < kPlanes; ++pl)
+                o[i > 0] = mma(zf[(i == 2 ? 2 : 0) + hf], *reinterpret_cast<const Operand<T> *>(pairs + ((2 * i + hf) * kPlanes + pl) * 1024 + 16 * lane), o[i > 0]);
+        } else {
+          Operand<T> pw[2][kPlanes];
+          pairs_of(I0{}, I0{}, y_along, pw);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) sc = mma(Tl::along(y_along, sb, ks), xf[tb][ks], sc);
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              float w[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int v = 8 * hf + e, gap = 32 * (tb - sb) + l32 - mfma_row(v, g);
-                const float r = sc[v] * (rel[32 + gap] * a.scale);
-                w[e] = tb > sb || gap >= 0 ? r : 0.f;
-              }
-              Operand<T> pw;
-              to_operand(w, pw);
-              o[tb] = mma(zf[2 * sb + hf], pw, o[tb]);
-            }
-          }
-        __builtin_amdgcn_sched_barrier(0);
+          for (int hf = 0; hf < 2; ++hf) o[0] = mma(zf[hf], pw[hf][0], o[0]);
+        }
         if (kMany ? last : true) {
           constexpr int es = (int)sizeof(T);
+          stored = nv == C;
 #pragma unroll
           for (int tb = 0; tb < TB; ++tb) {
             const int i = 32 * tb + l32;
             if (i < nv) {
               const int64_t row = kRev ? n - 1 - (c0 + i) : c0 + i;
-              char *dst = ob + row * a.o_t + (kMany ? 0 : hd * a.o_h) + (32 * wave + 4 * g) * es;
+              char *dst = ob + row * a.o_t + (kMany ? 0 : hd * a.o_h) + (32 * wave + 8 * g) * es;
 #pragma unroll
-              for (int vq = 0; vq < 4; ++vq) {
-                if constexpr (Tl::kBf16)
-                  *reinterpret_cast<uint2 *>(dst + 8 * vq * es) =
-                      make_uint2(pack_bf16(o[tb][4 * vq], o[tb][4 * vq + 1]), pack_bf16(o[tb][4 * vq + 2], o[tb][4 * vq + 3]));
-                else
-                  *reinterpret_cast<float4 *>(dst + 8 * vq * es) =
-                      make_float4(o[tb][4 * vq], o[tb][4 * vq + 1], o[tb][4 * vq + 2], o[tb][4 * vq + 3]);
+              for (int hf = 0; hf < 2; ++hf) {
+                const f32x16 &x = o[tb];
+                const int v = 8 * hf;
+                if constexpr (Tl::kBf16) {
+                  *reinterpret_cast<uint4 *>(dst + 16 * hf * es) = make_uint4(pack_bf16(x[v], x[v + 1]), pack_bf16(x[v + 2], x[v + 3]),
+                                                                              pack_bf16(x[v + 4], x[v + 5]), pack_bf16(x[v + 6], x[v + 7]));
+                } else {
+                  *reinterpret_cast<float4 *>(dst + 16 * hf * es) = make_float4(x[v], x[v + 1], x[v + 2], x[v + 3]);
+                  *reinterpret_cast<float4 *>(dst + 16 * hf * es + 16) = make_float4(x[v + 4], x[v + 5], x[v + 6], x[v + 7]);
+                }
               }
             }
           }
@@ -255,10 +296,14 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
       }
       if (kMany || last) {   // the state behind the chunk
         if (kMany ? hd == 0 : true) {
+          carry += lam_lo;
+          float f = lam_hi + carry;
+          carry -= f - lam_hi;
+          if (nv < C) f = (float)exp((double)al * nv);
 #pragma unroll
           for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) S[blk][v] = fmaf(S[blk][v], lam_hi, S[blk][v] * lam_lo);
+            for (int v = 0; v < 16; ++v) S[blk][v] *= f;
         }
 #pragma unroll
         for (int ks = 0; ks < SK; ++ks) {
@@ -270,13 +315,19 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
           const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
           for (int e = 0; e < 8; ++e) zs[e] *= w[e];
-          Operand<T> pl[kPlanesZ];
+          Operand<T> pl[kPlanesZ], yt[NB];
           split_operand<kPlanesZ>(zs, pl);
 #pragma unroll
           for (int blk = 0; blk < NB; ++blk) {
-            const Operand<T> yt = Tl::across(y_across, blk, ks);
+            yt[blk] = Tl::across(y_across, blk, ks);
+            S[blk] = mma(yt[blk], pl[0], S[blk]);
+            if constexpr (kPlanesZ > 1) S[blk] = mma(yt[blk], pl[1], S[blk]);
+          }
+          if constexpr (kPlanesZ > 2) {
+            if (a.fine_state) {
 #pragma unroll
-            for (int i = 0; i < kPlanesZ; ++i) S[blk] = mma(yt, pl[i], S[blk]);
+              for (int blk = 0; blk < NB; ++blk) S[blk] = mma(yt[blk], pl[2], S[blk]);
+            }
           }
         }
       }
@@ -298,7 +349,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
     for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        dst[(32 * blk + 16 * (v >> 3) + 8 * g + (v & 7)) * D + 32 * wave + l32] = f * S[blk][v];
+        dst[(32 * blk + 16 * (v >> 3) + 8 * g + (v & 7)) * D + 32 * wave + zl] = f * S[blk][v];
   }
 }
 
@@ -430,22 +481,30 @@ size_t state_bytes(const kvm_linear_config *c) {
   return (size_t)c->batch * c->n_kv_heads * c->head_dim * c->head_dim * sizeof(float);
 }
 
-template <typename T, int D, bool kRev, bool kMany, bool kOut>
+template <typename T, int D, bool kRev, bool kMany, bool kOut, bool kFine>
 hipError_t launch_walk_as(const LinArgs &a, int n_wg, hipStream_t st) {
   static OncePerDevice<hipError_t> once;
-  constexpr size_t bytes = linear_lds<T, D>();
-  hipError_t e = allow_lds(once, (const void *)linear_walk_kernel<T, D, kRev, kMany, kOut>, bytes);
+  constexpr size_t bytes = linear_lds<T, D, kFine>();
+  hipError_t e = allow_lds(once, (const void *)linear_walk_kernel<T, D, kRev, kMany, kOut, kFine>, bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((linear_walk_kernel<T, D, kRev, kMany, kOut>), dim3((unsigned)n_wg), dim3(2 * D), bytes, st, a);
+  hipLaunchKernelGGL((linear_walk_kernel<T, D, kRev, kMany, kOut, kFine>), dim3((unsigned)n_wg), dim3(2 * D), bytes, st, a);
   return hipGetLastError();
 }
+// Prompts of up to kFineTokens tokens are a few chunks long and wait for latencies: two more operands for each product cost
+// them nothing that shows.  Longer ones have many pairs behind most outputs, and the roundings of these average out.
+constexpr int kFineTokens = 128;
 template <bool kRev, bool kMany, bool kOut>
 hipError_t launch_walk(const kvm_linear_config *c, const LinArgs &a, int n_wg, hipStream_t st) {
-  if (c->io_dtype == KVM_BF16)
-    return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut>(a, n_wg, st)
-                              : launch_walk_as<bf16_t, 64, kRev, kMany, kOut>(a, n_wg, st);
-  return c->head_dim == 128 ? launch_walk_as<float, 128, kRev, kMany, kOut>(a, n_wg, st)
-                            : launch_walk_as<float, 64, kRev, kMany, kOut>(a, n_wg, st);
+  if (c->io_dtype == KVM_F32)
+    return c->head_dim == 128 ? launch_walk_as<float, 128, kRev, kMany, kOut, false>(a, n_wg, st)
+                              : launch_walk_as<float, 64, kRev, kMany, kOut, false>(a, n_wg, st);
+  if constexpr (kOut) {
+    if (a.T <= kFineTokens)
+      return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut, true>(a, n_wg, st)
+                                : launch_walk_as<bf16_t, 64, kRev, kMany, kOut, true>(a, n_wg, st);
+  }
+  return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut, false>(a, n_wg, st)
+                            : launch_walk_as<bf16_t, 64, kRev, kMany, kOut, false>(a, n_wg, st);
 }
 hipError_t launch_segments(const kvm_linear_config *c, const LinArgs &a, hipStream_t st) {
   const int dd = c->head_dim * c->head_dim;
@@ -505,7 +564,7 @@ extern "C" int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, c
   a.y_b = s.k_b * es; a.y_t = s.k_t * es; a.y_h = s.k_h * es;
   a.z_b = s.v_b * es; a.z_t = s.v_t * es; a.z_h = s.v_h * es;
   a.o_b = s.o_b * es; a.o_t = s.o_t * es; a.o_h = s.o_h * es;
-  a.log_decay = log_decay; a.lens = lens; a.start = state_in; a.seg = (float *)workspace; a.end = state_out;
+  a.log_decay = log_decay; a.lens = lens; a.start = state_in; a.seg = (float *)workspace; a.end = state_out; a.fine_state = state_out != nullptr;
   a.start_scale = a.end_scale = 1.f; a.scale = scale_of(cfg);
   a.T = (int32_t)T; a.H = (int32_t)hk; a.G = (int32_t)(hq / hk); a.units = cfg->batch * cfg->n_kv_heads;
   a.n_seg = cut.n_seg; a.seg_tokens = cut.seg_tokens;
@@ -565,7 +624,7 @@ extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, 
   if (e == hipSuccess) e = launch_walk<false, false, true>(cfg, a, a.units * a.n_seg, st);
   // dv and dk: backwards; the state there is that of the products q dout, without the scale
   LinArgs r = roles(k, false, q, true, dout, true, dv);
-  r.start = dstate_out; r.start_scale = 1.f / scale; r.end = dstate_in; r.end_scale = scale;
+  r.start = dstate_out; r.start_scale = 1.f / scale; r.end = dstate_in; r.end_scale = scale; r.fine_state = dstate_in != nullptr;
   if (cut.n_seg > 1) {
     if (e == hipSuccess) e = launch_walk<true, true, false>(cfg, r, r.units * (r.n_seg - 1), st);
     if (e == hipSuccess) e = launch_segments(cfg, r, st);

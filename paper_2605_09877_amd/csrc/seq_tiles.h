@@ -95,18 +95,31 @@ struct Tile {
 
   // Rows 0 .. kRows - 1 of the tile at LDS address `at`, by kNW waves.  base (wave-uniform): the first of nv >= 1 rows in
   // memory, `stride` bytes apart; kRev: tile row r is memory row nv - 1 - r.  Tile rows beyond the last repeat it.
+  // (swz is linear in the bits of a row: a lane's chunk is its own of the first piece, exclusive or the piece's)
   template <int kRows, int kNW, bool kRev>
   __device__ static __forceinline__ void fill(const char *base, uint32_t stride, int nv, uint32_t at, int wave, int lane) {
     constexpr int kPer = kRows / kPieceRows / kNW;
     static_assert(kPer * kNW * kPieceRows == kRows, "waves share a tile evenly");
-    const uint32_t rl = (uint32_t)(16 * lane) / kRowB, slot = (uint32_t)lane % (kRowB / 16);
+    const uint32_t rl = (uint32_t)(16 * lane) / kRowB, col = 16 * (((uint32_t)lane % (kRowB / 16)) ^ swz(rl));
+    const uint32_t piece0 = (uint32_t)(wave * kPer);
+    if (nv >= kRows) {
+      const uint32_t row = (kRev ? kPieceRows - 1 - rl : rl) * stride;
+      base += (kRev ? kRows - (piece0 + 1) * kPieceRows : piece0 * kPieceRows) * stride;
 #pragma unroll
-    for (int n = 0; n < kPer; ++n) {
-      const uint32_t piece = (uint32_t)(wave * kPer + n);
-      const int r = (int)(piece * kPieceRows + rl);
-      int m = kRev ? nv - 1 - r : r;
-      m = m < 0 ? 0 : m < nv ? m : nv - 1;
-      dma16(base, (uint32_t)m * stride + 16 * (slot ^ swz((uint32_t)r)), at + piece * 1024u);
+      for (int n = 0; n < kPer; ++n) {
+        const uint32_t piece = piece0 + n;
+        dma16(base, row + (col ^ (16 * swz(piece * kPieceRows))), at + piece * 1024u);
+        base = kRev ? base - kPieceRows * stride : base + kPieceRows * stride;
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < kPer; ++n) {
+        const uint32_t piece = piece0 + n;
+        const int r = (int)(piece * kPieceRows + rl);
+        int m = kRev ? nv - 1 - r : r;
+        m = m < 0 ? 0 : m < nv ? m : nv - 1;
+        dma16(base, (uint32_t)m * stride + (col ^ (16 * swz(piece * kPieceRows))), at + piece * 1024u);
+      }
     }
   }
 
@@ -166,6 +179,16 @@ struct Tile {
     return o;
   }
 };
+
+// Waits of loops that fill tiles with direct loads while stores of earlier results are under way.  wait_vmem<N>: until N of the
+// wave's vector memory operations are left (they end in order).  publish: a barrier that waits for LDS operations alone.
+template <int N>
+__device__ __forceinline__ void wait_vmem() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void publish() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 
 // An address computed where it is used: kept out of registers between uses (loops short of registers).
 __device__ __forceinline__ uint32_t here(uint32_t x) {

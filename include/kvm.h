@@ -429,11 +429,12 @@ int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, const void *
                        const kvm_strides *strides, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Gradients of a loss with respect to q, k, v and state_in of that call (dense), from dout, the gradient with respect to its out,
- * and dstate_out, that with respect to its state_out (NULL: none).  dstate_in may be NULL.  Rows behind a sequence get zero. */
+ * and dstate_out, that with respect to its state_out (NULL: none).  dstate_in may be NULL.  Rows behind a sequence get zero.
+ * kept: the workspace of that call as it left it (it is read, and saves forming the states again), or NULL. */
 int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, const void *k, const void *v, const float *log_decay,
                         const float *state_in, const int32_t *lens, const void *dout, const float *dstate_out, void *dq,
-                        void *dk, void *dv, float *dstate_in, int64_t T, void *workspace, size_t workspace_bytes,
-                        void *stream);
+                        void *dk, void *dv, float *dstate_in, int64_t T, const void *kept, void *workspace,
+                        size_t workspace_bytes, void *stream);
 
 /* One token per sequence: the state is advanced in place and asked.  q, out: [B, H_q, d]; k, v: [B, H_kv, d], dense;
  * active: nullable device int32 [B]; a sequence whose entry is 0 keeps its state and gets zeros. */

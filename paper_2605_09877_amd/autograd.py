@@ -65,8 +65,9 @@ class _LinearAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, log_decay, state, lens, scale):
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
-        out, end = linear_prefill(q, k, v, log_decay, state=state, lens=lens, scale=scale)
-        ctx.save_for_backward(q, k, v, log_decay, state, lens)
+        keep = []
+        out, end = linear_prefill(q, k, v, log_decay, state=state, lens=lens, scale=scale, keep=keep)
+        ctx.save_for_backward(q, k, v, log_decay, state, lens, *keep)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
         return out, end
@@ -74,11 +75,11 @@ class _LinearAttention(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, dend):
-        q, k, v, log_decay, state, lens = ctx.saved_tensors
+        q, k, v, log_decay, state, lens, kept = ctx.saved_tensors
         dout = torch.zeros_like(q) if dout is None else dout.contiguous()
         dend = None if dend is None else dend.contiguous()
         dq, dk, dv, dstate = linear_backward(q, k, v, log_decay, dout, state=state, dstate_out=dend, lens=lens, scale=ctx.scale,
-                                             want_dstate=state is not None and ctx.needs_input_grad[4])
+                                             want_dstate=state is not None and ctx.needs_input_grad[4], kept=kept)
         return dq, dk, dv, None, dstate, None, None
 
 

@@ -136,7 +136,7 @@ def load_library() -> C.CDLL:
     lib.kvm_linear_workspace_bytes.restype = C.c_size_t
     lib.kvm_linear_workspace_bytes.argtypes = [lin, i64]
     lib.kvm_linear_prefill.argtypes = [lin] + [vp] * 8 + [i64, C.POINTER(kvm_strides), vp, C.c_size_t, vp]
-    lib.kvm_linear_backward.argtypes = [lin] + [vp] * 12 + [i64, vp, C.c_size_t, vp]
+    lib.kvm_linear_backward.argtypes = [lin] + [vp] * 12 + [i64, vp, vp, C.c_size_t, vp]
     lib.kvm_linear_decode.argtypes = [lin] + [vp] * 8
     win = C.POINTER(kvm_window_config)
     lib.kvm_window_prefill.argtypes = [win] + [vp] * 7 + [i64, i64, C.POINTER(kvm_strides), vp]
@@ -660,11 +660,12 @@ def _linear_config(q, k, scale) -> kvm_linear_config:
     return kvm_linear_config(q.shape[0], Hq, Hkv, d, _io_of(q), 0.0 if scale is None else float(scale))
 
 
-def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional[float] = None, out=None, state_out=None):
+def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional[float] = None, out=None, state_out=None,
+                   keep: Optional[list] = None):
     """kvm_linear_prefill: linear attention with a decay for each KV head over T tokens of every sequence.
     q [B,T,Hq,d]; k, v [B,T,Hkv,d] (bf16 or fp32; views whose head_dim is contiguous); log_decay fp32 [Hkv];
     state fp32 [B,Hkv,d,d], what a call before has left, or None (zero); lens int32 [B], the sequences' lengths in a padded batch.
-    Returns (out, state_out); state_out may be `state` itself."""
+    Returns (out, state_out); state_out may be `state` itself.  keep: a list that is given the call's workspace, for linear_backward."""
     lib = load_library()
     cfg = _linear_config(q, k, scale)
     B, T = q.shape[:2]
@@ -687,12 +688,15 @@ def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional
         status = lib.kvm_linear_prefill(cfg, *ptrs, T, _row_strides(q, k, v, out), ws.data_ptr(), nbytes, _stream())
     if status != KVM_OK:
         _check(status, "kvm_linear_prefill")
+    if keep is not None:
+        keep.append(ws)
     return out, state_out
 
 
 def linear_backward(q, k, v, log_decay, dout, *, state=None, dstate_out=None, lens=None, scale: Optional[float] = None,
-                    want_dstate: bool = False):
-    """kvm_linear_backward: (dq, dk, dv, dstate or None) of a linear_prefill over these tensors (contiguous)."""
+                    want_dstate: bool = False, kept=None):
+    """kvm_linear_backward: (dq, dk, dv, dstate or None) of a linear_prefill over these tensors (contiguous).  kept: what that call
+    put into its `keep` list, or None."""
     lib = load_library()
     cfg = _linear_config(q, k, scale)
     B, T = q.shape[:2]
@@ -711,7 +715,8 @@ def linear_backward(q, k, v, log_decay, dout, *, state=None, dstate_out=None, le
         raise KVMError(KVM_ERR_ARG, "kvm_linear_workspace_bytes: unsupported sizes")
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     with _on_device(dev):
-        status = lib.kvm_linear_backward(cfg, *ptrs, T, ws.data_ptr(), nbytes, _stream())
+        status = lib.kvm_linear_backward(cfg, *ptrs, T, _want(kept, (nbytes,), torch.uint8, dev, "kept"), ws.data_ptr(), nbytes,
+                                         _stream())
     if status != KVM_OK:
         _check(status, "kvm_linear_backward")
     return dq, dk, dv, dstate

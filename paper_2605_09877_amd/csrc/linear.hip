@@ -162,8 +162,10 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   auto pairs_of = [&](auto tb_, auto sb_, uint32_t y_along, Operand<T> (&pw)[2][kPlanes]) {
     constexpr int tb = decltype(tb_)::value, sb = decltype(sb_)::value;
     f32x16 sc = {0.f};
+    // (many heads of y: x is in registers for the first of them alone, where the state is asked)
+    const uint32_t x = kMany && kShare ? here(at_x + lane_along) : 0;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sc = mma(Tl::along(y_along, sb, ks), xf[tb][ks], sc);
+    for (int ks = 0; ks < KS; ++ks) sc = mma(Tl::along(y_along, sb, ks), kMany && kShare ? Tl::along(x, tb, ks) : xf[tb][ks], sc);
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       float w[8];
@@ -365,13 +367,22 @@ __global__ __launch_bounds__(256) void linear_segments_kernel(LinArgs a, int dd)
     s = *reinterpret_cast<const float4 *>(a.start + (int64_t)u * dd + i);
     s.x *= a.start_scale; s.y *= a.start_scale; s.z *= a.start_scale; s.w *= a.start_scale;
   }
+  // segments that another one follows are full; eight of them are asked for at a time
+  const int n_full = n > 0 ? (n - 1) / a.seg_tokens : -1;
   float *at = a.seg + (int64_t)u * a.n_seg * dd + i;
-  for (int seg = 0; seg < a.n_seg; ++seg, at += dd) {
-    if ((int64_t)seg * a.seg_tokens >= n) break;
-    const bool full = (int64_t)(seg + 1) * a.seg_tokens < n;   // another one follows
-    const float4 add = full ? *reinterpret_cast<const float4 *>(at) : make_float4(0.f, 0.f, 0.f, 0.f);
-    *reinterpret_cast<float4 *>(at) = s;
-    s.x = fmaf(s.x, lam, add.x); s.y = fmaf(s.y, lam, add.y); s.z = fmaf(s.z, lam, add.z); s.w = fmaf(s.w, lam, add.w);
+  constexpr int kAhead = 8;
+  for (int seg0 = 0; seg0 <= n_full; seg0 += kAhead) {
+    float4 add[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (seg0 + k < n_full) add[k] = *reinterpret_cast<const float4 *>(at + (int64_t)(seg0 + k) * dd);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (seg0 + k <= n_full) *reinterpret_cast<float4 *>(at + (int64_t)(seg0 + k) * dd) = s;
+      if (seg0 + k < n_full) {
+        s.x = fmaf(s.x, lam, add[k].x); s.y = fmaf(s.y, lam, add[k].y); s.z = fmaf(s.z, lam, add[k].z); s.w = fmaf(s.w, lam, add[k].w);
+      }
+    }
   }
 }
 
@@ -462,8 +473,9 @@ bool valid(const kvm_linear_config *c) {
 }
 float scale_of(const kvm_linear_config *c) { return c->scale > 0.f ? c->scale : 1.f / sqrtf((float)c->head_dim); }
 
-// Segments a sequence is cut into: one workgroup has one segment of one unit, and the device holds kFill of them
-// at once.  The first pass reads y and z once more, so a segment has 8 chunks at least.
+// Segments a sequence is cut into: one workgroup has one segment of one unit, and the device holds `fill` of them at once.  The
+// first pass reads y and z once more, so there are no more than it takes to fill the device; a segment has two chunks at
+// least, and sequences of fewer than eight chunks are not cut (two more launches cost more than the chunks walked less).
 struct Cut {
   int n_seg, seg_tokens;
 };
@@ -472,8 +484,8 @@ Cut cut_of(const kvm_linear_config *c, int64_t T) {
   const int64_t units = (int64_t)c->batch * c->n_kv_heads, chunks = (T + chunk - 1) / chunk;
   const int64_t fill = c->head_dim == 128 ? 512 : 1024;
   int64_t n = (fill + units - 1) / units;
-  if (n > chunks / 8) n = chunks / 8;
-  if (n < 1) n = 1;
+  if (n > chunks / 2) n = chunks / 2;
+  if (n < 1 || chunks < 8) n = 1;
   const int64_t per = (chunks + n - 1) / n;
   return Cut{(int)((chunks + per - 1) / per), (int)(per * chunk)};
 }
@@ -581,11 +593,11 @@ extern "C" int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, c
 extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, const void *k, const void *v,
                                    const float *log_decay, const float *state_in, const int32_t *lens, const void *dout,
                                    const float *dstate_out, void *dq, void *dk, void *dv, float *dstate_in, int64_t T,
-                                   void *workspace, size_t workspace_bytes, void *stream) {
+                                   const void *kept, void *workspace, size_t workspace_bytes, void *stream) {
   using namespace kvm;
   if (!valid(cfg) || T <= 0 || T >= (1ll << 31) || !q || !k || !v || !log_decay || !dout || !dq || !dk || !dv || !workspace)
     return KVM_ERR_ARG;
-  const void *ptrs[] = {q, k, v, state_in, dout, dstate_out, dq, dk, dv, dstate_in, workspace};
+  const void *ptrs[] = {q, k, v, state_in, dout, dstate_out, dq, dk, dv, dstate_in, kept, workspace};
   for (const void *x : ptrs)
     if (!al16(x)) return KVM_ERR_ARG;
   if (workspace_bytes < kvm_linear_workspace_bytes(cfg, T)) return KVM_ERR_CAPACITY;
@@ -615,12 +627,13 @@ extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, 
   // dq: the forward walk's states, transposed
   LinArgs f = roles(q, true, k, false, v, false, dq);
   f.start = state_in; f.start_scale = f.end_scale = 1.f;
-  if (cut.n_seg > 1) {
+  if (cut.n_seg > 1 && !kept) {
     e = launch_walk<false, false, false>(cfg, f, f.units * (f.n_seg - 1), st);
     if (e == hipSuccess) e = launch_segments(cfg, f, st);
   }
   LinArgs a = roles(dout, true, v, false, k, false, dq);
   a.start = state_in; a.start_scale = 1.f; a.transposed = 1;
+  if (kept) a.seg = (float *)const_cast<void *>(kept);   // (read alone)
   if (e == hipSuccess) e = launch_walk<false, false, true>(cfg, a, a.units * a.n_seg, st);
   // dv and dk: backwards; the state there is that of the products q dout, without the scale
   LinArgs r = roles(k, false, q, true, dout, true, dv);

@@ -7,6 +7,8 @@
 //   S^T[key, query] = K Q^T,  P^T = 2^(S^T scale log2 e - m),  O^T[channel, query] += V^T P^T
 #include <math.h>
 
+#include <type_traits>
+
 #include "../../include/kvm.h"
 #include "kvm_internal.h"
 #include "seq_tiles.h"
@@ -30,7 +32,7 @@ struct WinArgs {
   const int32_t *lens;   // nullable
   float scale;
   int32_t B, Hq, Hkv, Tq, Tk, W, S;
-  int32_t by_head, tiles, per_block, blocks;   // position tiles, of which per_block make a block; blocks of a unit
+  int32_t by_head, span, tiles, per_block, blocks;   // position tiles, of which per_block make a block; blocks of a unit
   // backward
   const char *dout;
   char *dq, *dk, *dv;
@@ -41,7 +43,9 @@ struct WinArgs {
 };
 
 template <typename T, int D>
-constexpr int kTileRows = D * (int)sizeof(T) <= 256 ? 64 : 32;   // keys of a tile: 16 KiB at most
+constexpr int kTileRows = D * (int)sizeof(T) <= 256 ? 64 : 32;   // keys of a tile in the dq kernel: 16 KiB at most
+template <typename T, int D>
+constexpr int kPromptRows = D * (int)sizeof(T) <= 128 ? 64 : 32;   // in the prompt kernel
 
 __device__ __forceinline__ int tokens_of(const WinArgs &a, int b) {
   int n = a.Tk;
@@ -127,24 +131,128 @@ __device__ __forceinline__ void load4(const char *row, int blk, int vq, int g, f
   }
 }
 
+// A query done again, one visible key after the other in fp32 (a lane has half of its channels): a key that it does not see
+// enters the second product of the tile kernels with p = 0, and a value of it that is not finite makes that NaN.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
+__device__ __forceinline__ void attend_one_by_one(const WinArgs &a, const char *qrow, const char *kb, const char *vb, int t, float c,
+                                                  int g, f32x16 (&o)[D / 32], float &m, float &l) {
+  constexpr int DB = D / 32;
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
+  m = -INFINITY;
+  l = 0.f;
+#pragma unroll 1
+  for (int j = 0; j <= t; ++j) {
+    if (j >= a.S && t - j >= a.W) {
+      j = t - a.W;   // (the next one is the window's first)
+      continue;
+    }
+    const char *kr = kb + (int64_t)j * a.k_t, *vr = vb + (int64_t)j * a.v_t;
+    float dot = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < 4 * DB; ++i) {
+      float x[4], y[4];
+      load4<T>(qrow, i >> 2, i & 3, g, x);
+      load4<T>(kr, i >> 2, i & 3, g, y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dot = fmaf(x[e], y[e], dot);
+    }
+    const float x = xhalf_sum(dot) * c, m_new = fmaxf(m, x);
+    if (m_new == -INFINITY) continue;
+    const float alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(x - m_new);
+    m = m_new;
+    l = fmaf(l, alpha, p);
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      float y[4];
+      load4<T>(vr, i >> 2, i & 3, g, y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i >> 2][4 * (i & 3) + e] = fmaf(p, y[e], o[i >> 2][4 * (i & 3) + e] * alpha);
+    }
+  }
+}
+
+// What a query's lane pair has in the end: o / l to out, what its rounding leaves to rest, the logarithm of the sum to lse.
+template <typename T, int D>
+__device__ __forceinline__ void write_query(const WinArgs &a, char *orow, float *lse, const f32x16 (&o)[D / 32], float m, float l, int g) {
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // (l = 0: every logit is -infinity)
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) {
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = o[i >> 2][4 * (i & 3) + e] * inv;
+    store4<T>(orow, i >> 2, i & 3, g, x[0], x[1], x[2], x[3]);
+    if constexpr (sizeof(T) == 2) {
+      if (a.rest) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] -= __uint_as_float((uint32_t)float_to_bf16_bits(x[e]) << 16);
+        store4<T>(a.rest + (orow - a.out), i >> 2, i & 3, g, x[0], x[1], x[2], x[3]);
+      }
+    }
+  }
+  if (lse && g == 0) *lse = (m + log2f(l)) * kLn2;
+}
+template <typename T, int D>
+__device__ __forceinline__ bool all_finite(const f32x16 (&o)[D / 32], float l) {
+  float bad = 0.f * l;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bad = fmaf(o[i][v], 0.f, bad);
+  return xhalf_sum(bad) == 0.f;
+}
+
+// Operands of two tiles, one read along its rows (K) and one across (V), whose addresses stay in registers: the step's and the
+// buffer's parts are constants that fold into the instructions.
+template <typename T, int D>
+struct Fragments {
   using Tl = Tile<T, D>;
-  constexpr int KT = kTileRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  static constexpr int kAlong = D / 16, kAcross = D / 32, kN = sizeof(T) == 2 ? 2 : 8;
+  uint32_t al[kAlong], ac[kAcross][sizeof(T) == 2 ? 2 : 1];
+  __device__ __forceinline__ Fragments(uint32_t at_k, uint32_t at_v, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < kAlong; ++ks) al[ks] = (at_k + Tl::along0(lane)) ^ (uint32_t)(16 * (int)sizeof(T) * ks);
+#pragma unroll
+    for (int blk = 0; blk < kAcross; ++blk)
+#pragma unroll
+      for (int hi = 0; hi < (sizeof(T) == 2 ? 2 : 1); ++hi)
+        ac[blk][hi] = (at_v + Tl::template across0<true>(lane)) ^ (uint32_t)(32 * (int)sizeof(T) * blk + 32 * hi);
+  }
+  __device__ __forceinline__ Operand<T> along(int blk, int ks, uint32_t buf) const {
+    return Tl::along(al[ks] + buf, blk, 0);
+  }
+  __device__ __forceinline__ Operand<T> across(int blk, int ks, uint32_t buf) const {
+    if constexpr (sizeof(T) == 2) {
+      Operand<T> o;
+#pragma unroll
+      for (int hi = 0; hi < 2; ++hi)
+        o.f.d[hi] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                  (__attribute__((address_space(3))) v4i16 *)(uintptr_t)(ac[blk][hi] + buf + (uint32_t)((16 * ks + 8 * hi) * Tl::kRowB))));
+      return o;
+    } else {
+      return Tl::across(ac[blk][0] + buf, 0, ks);
+    }
+  }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 2) void window_prefill_kernel(WinArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int KT = kPromptRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = KT * Tl::kRowB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t at_k = lds_addr_of(lds), at_v = at_k + 2 * kTileB;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
-  const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<true>(lane);
   const Item w(a);
   if (w.none) return;
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
   const int n = tokens_of(a, w.b);
-  const int span = a.by_head ? 32 : 32 * kWaves;
   const int nq = n - off < 0 ? 0 : n - off;                           // queries of the sequence (n <= Tk: at most Tq)
-  const int Q0 = w.tile * span, Q1 = Q0 + span < nq ? Q0 + span : nq;  // the workgroup's
+  const int Q0 = w.tile * a.span, Q1 = Q0 + a.span < nq ? Q0 + a.span : nq;  // the workgroup's
   const int hq = w.hkv * G + w.head + (a.by_head ? wave : 0);
   const int myq = Q0 + (a.by_head ? 0 : 32 * wave) + l32;
   char *orow = a.out + w.b * a.o_b + (int64_t)myq * a.o_t + (int64_t)hq * a.o_h;
@@ -179,33 +287,31 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
     for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
   float m = -INFINITY, l = 0.f;
   const int wt0 = off + Q0 + (a.by_head ? 0 : 32 * wave);   // position of the wave's first query
-  __builtin_amdgcn_s_waitcnt(0);
-  load_tile(0);
-  for (int it = 0; it < keys.n_tiles; ++it) {
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (it + 1 < keys.n_tiles) load_tile(it + 1);
+  // LDS addresses of the lane's fragments, but for constants
+  const Fragments<T, D> fr(at_k, at_v, lane);
+  const int n_tiles = __builtin_amdgcn_readfirstlane(keys.n_tiles);
+  auto tile_step = [&](int it, auto parity) {
+    constexpr uint32_t kBuf = decltype(parity)::value * kTileB;
+    wait_vmem<0>();
+    publish();
+    if (it + 1 < n_tiles) load_tile(it + 1);
     const int j0 = keys.first(it, KT), j1 = keys.end(it);
-    if (j0 > wt0 + 31) continue;   // all behind the wave's queries
-    const uint32_t kt = at_k + (uint32_t)(it & 1) * kTileB, vt = at_v + (uint32_t)(it & 1) * kTileB;
+    if (j0 > wt0 + 31) return;   // all behind the wave's queries
     f32x16 s[NB];
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) s[blk][v] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int blk = 0; blk < NB; ++blk) s[blk] = mma(Tl::along(kt + lane_along, blk, ks), qf[ks], s[blk]);
+      for (int blk = 0; blk < NB; ++blk) s[blk] = mma(fr.along(blk, ks, kBuf), qf[ks], ks == 0 ? f32x16{0.f} : s[blk]);
     // every pair is visible: keys j0 .. j0 + KT - 1 up to the first query's position and inside the last one's window
     if (!(j0 + KT <= j1 && j0 + KT - 1 <= wt0 && (wt0 + 31 - j0 < a.W || j0 + KT <= a.S))) {
+      // of the lane's tile rows, those up to `last` are visible, and of them those from `first` on or below `sink`
+      const int last = (t < j1 - 1 ? t : j1 - 1) - j0 - 4 * g, first = t - a.W + 1 - j0 - 4 * g, sink = a.S - j0 - 4 * g;
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const int j = j0 + 32 * blk + mfma_row(v, g);
-          const bool sees = j < j1 && j <= t && (t - j < a.W || j < a.S);
-          s[blk][v] = sees ? s[blk][v] : -INFINITY;
+          const int r = 32 * blk + mfma_row(v, 0);
+          s[blk][v] = r <= last && (r >= first || r < sink) ? s[blk][v] : -INFINITY;
         }
     }
     float top = s[0][0];
@@ -228,16 +334,12 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
     }
     const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen yet)
 #pragma unroll
-    for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) s[blk][v] = __builtin_amdgcn_exp2f(fmaf(s[blk][v], c, -ref));
-#pragma unroll
     for (int ks = 0; ks < 2 * NB; ++ks) {
       // P enters the second product in the I/O dtype; the sum is taken over the rounded values, so that numerator and
       // denominator see the same ones
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = s[ks >> 1][8 * (ks & 1) + e];
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + e], c, -ref));
       Operand<T> pf;
       to_operand(p, pf);
       if constexpr (sizeof(T) == 2) {
@@ -249,77 +351,25 @@ __global__ __launch_bounds__(256, 2) void window_prefill_kernel(WinArgs a) {
         for (int e = 0; e < 8; ++e) l += p[e];
       }
 #pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] = mma(Tl::across(vt + lane_across, i, ks), pf, o[i]);
+      for (int i = 0; i < DB; ++i) o[i] = mma(fr.across(i, ks, kBuf), pf, o[i]);
     }
+  };
+  __builtin_amdgcn_s_waitcnt(0);
+  load_tile(0);
+  for (int it = 0; it < n_tiles; it += 2) {
+    tile_step(it, std::integral_constant<uint32_t, 0>{});
+    if (it + 1 < n_tiles) tile_step(it + 1, std::integral_constant<uint32_t, 1>{});
   }
   l = xhalf_sum(l);
   if (myq >= nq) return;
-  // A key that a query does not see enters the second product with p = 0, and a value of it that is not finite makes that NaN: a
-  // query whose result is not finite is done again, one visible key after the other.
-  float bad = 0.f * l;
-#pragma unroll
-  for (int i = 0; i < DB; ++i)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) bad = fmaf(o[i][v], 0.f, bad);
-  if (!(xhalf_sum(bad) == 0.f)) {
-    const char *qrow = a.q + w.b * a.q_b + (int64_t)myq * a.q_t + (int64_t)hq * a.q_h;
-#pragma unroll
-    for (int i = 0; i < DB; ++i)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
-    m = -INFINITY;
-    l = 0.f;
-#pragma unroll 1
-    for (int j = 0; j <= t; ++j) {
-      if (j >= a.S && t - j >= a.W) {
-        j = t - a.W;   // (the next one is the window's first)
-        continue;
-      }
-      const char *kr = kb + (int64_t)j * a.k_t, *vr = vb + (int64_t)j * a.v_t;
-      float dot = 0.f;
-#pragma unroll 4
-      for (int i = 0; i < 4 * DB; ++i) {
-        float x[4], y[4];
-        load4<T>(qrow, i >> 2, i & 3, g, x);
-        load4<T>(kr, i >> 2, i & 3, g, y);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dot = fmaf(x[e], y[e], dot);
-      }
-      const float x = xhalf_sum(dot) * c, m_new = fmaxf(m, x);
-      if (m_new == -INFINITY) continue;
-      const float alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(x - m_new);
-      m = m_new;
-      l = fmaf(l, alpha, p);
-#pragma unroll
-      for (int i = 0; i < 4 * DB; ++i) {
-        float y[4];
-        load4<T>(vr, i >> 2, i & 3, g, y);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i >> 2][4 * (i & 3) + e] = fmaf(p, y[e], o[i >> 2][4 * (i & 3) + e] * alpha);
-      }
-    }
-  }
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // (l = 0: every logit is -infinity)
-#pragma unroll
-  for (int i = 0; i < 4 * DB; ++i) {
-    float x[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = o[i >> 2][4 * (i & 3) + e] * inv;
-    store4<T>(orow, i >> 2, i & 3, g, x[0], x[1], x[2], x[3]);
-    if constexpr (sizeof(T) == 2) {
-      if (a.rest) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] -= __uint_as_float((uint32_t)float_to_bf16_bits(x[e]) << 16);
-        store4<T>(a.rest + (orow - a.out), i >> 2, i & 3, g, x[0], x[1], x[2], x[3]);
-      }
-    }
-  }
-  if (lse && g == 0) *lse = (m + log2f(l)) * kLn2;
+  if (!all_finite<T, D>(o, l))
+    attend_one_by_one<T, D>(a, a.q + w.b * a.q_b + (int64_t)myq * a.q_t + (int64_t)hq * a.q_h, kb, vb, t, c, g, o, m, l);
+  write_query<T, D>(a, orow, lse, o, m, l, g);
 }
 
 // ------------------------------------------------------------------------------------------------
 // Gradients.  P = 2^(S scale log2 e - lse log2 e) is formed again; D = dout . out of a query, out with what its rounding left;
-//   dS = scale P (dP - D),  dq = dS K (queries stay, keys stream),  dk = dS^T q, dv = P^T dout (keys stay, queries stream).
+//   dS = P (dP - D),  dq = scale dS K (queries stay, keys stream),  dk = scale dS^T q, dv = P^T dout (keys stay, queries stream).
 // P and dS enter their products in the I/O dtype.
 // (a query all of whose logits are -infinity has nothing of any key: P = 0)
 __device__ __forceinline__ float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
@@ -334,14 +384,12 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
-  const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<true>(lane);
   const Item w(a);
   if (w.none) return;
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
   const int n = tokens_of(a, w.b);
-  const int span = a.by_head ? 32 : 32 * kWaves;
   const int nq = n - off < 0 ? 0 : n - off;
-  const int Q0 = w.tile * span, Q1 = Q0 + span < nq ? Q0 + span : nq;
+  const int Q0 = w.tile * a.span, Q1 = Q0 + a.span < nq ? Q0 + a.span : nq;
   const int hq = w.hkv * G + w.head + (a.by_head ? wave : 0);
   const int myq = Q0 + (a.by_head ? 0 : 32 * wave) + l32;
   const int64_t at_row = w.b * a.o_b + (int64_t)myq * a.o_t + (int64_t)hq * a.o_h;
@@ -402,34 +450,33 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
   const int wt0 = off + Q0 + (a.by_head ? 0 : 32 * wave);
-  __builtin_amdgcn_s_waitcnt(0);
-  for (int it = 0; it < keys.n_tiles; ++it) {
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (it + 1 < keys.n_tiles) load_tile(it + 1);
+  const Fragments<T, D> fr(at_k, at_k, lane);
+  const int n_tiles = __builtin_amdgcn_readfirstlane(keys.n_tiles);
+  auto tile_step = [&](int it, auto parity) {
+    constexpr uint32_t kBuf = decltype(parity)::value * kTileB;
+    wait_vmem<0>();
+    publish();
+    if (it + 1 < n_tiles) load_tile(it + 1);
     const int j0 = keys.first(it, KT), j1 = keys.end(it);
-    if (j0 > wt0 + 31) continue;
-    const uint32_t kt = at_k + (uint32_t)(it & 1) * kTileB, vt = at_v + (uint32_t)(it & 1) * kTileB;
+    if (j0 > wt0 + 31) return;
     const bool masked = !(j0 + KT <= j1 && j0 + KT - 1 <= wt0 && (wt0 + 31 - j0 < a.W || j0 + KT <= a.S));
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
       f32x16 s, dp;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = dp[v] = 0.f;
-#pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = mma(Tl::along(kt + lane_along, blk, ks), qf[ks], s);
-        dp = mma(Tl::along(vt + lane_along, blk, ks), df[ks], dp);
+        s = mma(fr.along(blk, ks, kBuf), qf[ks], ks == 0 ? f32x16{0.f} : s);
+        dp = mma(fr.along(blk, ks, kBuf + 2 * kTileB), df[ks], ks == 0 ? f32x16{0.f} : dp);
       }
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        bool sees = true;
-        if (masked) {
-          const int j = j0 + 32 * blk + mfma_row(v, g);
-          sees = j < j1 && j <= t && (t - j < a.W || j < a.S);
+      for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2)) * (dp[v] - delta);
+      if (masked) {
+        const int last = (t < j1 - 1 ? t : j1 - 1) - j0 - 4 * g, first = t - a.W + 1 - j0 - 4 * g, sink = a.S - j0 - 4 * g;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = 32 * blk + mfma_row(v, 0);
+          s[v] = r <= last && (r >= first || r < sink) ? s[v] : 0.f;
         }
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2));
-        s[v] = sees ? p * (dp[v] - delta) * a.scale : 0.f;
       }
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
@@ -439,15 +486,20 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
         Operand<T> ds;
         to_operand(x, ds);
 #pragma unroll
-        for (int i = 0; i < DB; ++i) o[i] = mma(Tl::across(kt + lane_across, i, 2 * blk + hf), ds, o[i]);
+        for (int i = 0; i < DB; ++i) o[i] = mma(fr.across(i, 2 * blk + hf, kBuf), ds, o[i]);
       }
     }
+  };
+  __builtin_amdgcn_s_waitcnt(0);
+  for (int it = 0; it < n_tiles; it += 2) {
+    tile_step(it, std::integral_constant<uint32_t, 0>{});
+    if (it + 1 < n_tiles) tile_step(it + 1, std::integral_constant<uint32_t, 1>{});
   }
   if (myq >= nq) return;
 #pragma unroll
   for (int i = 0; i < 4 * DB; ++i)
-    store4<T>(a.dq + at_row, i >> 2, i & 3, g, o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2],
-              o[i >> 2][4 * (i & 3) + 3]);
+    store4<T>(a.dq + at_row, i >> 2, i & 3, g, a.scale * o[i >> 2][4 * (i & 3)], a.scale * o[i >> 2][4 * (i & 3) + 1],
+              a.scale * o[i >> 2][4 * (i & 3) + 2], a.scale * o[i >> 2][4 * (i & 3) + 3]);
 }
 
 // dk and dv of 128 keys, 32 to a wave (K in registers, V in LDS); the queries that see them, head after head of the group, stream
@@ -464,11 +516,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
   constexpr uint32_t kTileB = 32 * Tl::kRowB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t at_s = lds_addr_of(lds), at_v = at_s + 4 * kTileB;   // stage: q tile, dout tile; then 128 rows of v
-  float *rows = reinterpret_cast<float *>(lds + 8 * kTileB);           // [stage][lse log2 e | D][32]
+  float *rows = reinterpret_cast<float *>(lds + 8 * kTileB);           // [stage][lse, in powers of two | D][32]
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
-  const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<true>(lane);
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq, units = a.B * a.Hkv;
   const int per_unit = a.key_tiles + a.n_split;
   // a unit's workgroups go to one XCD
@@ -509,18 +560,19 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
     const char *qb = uniform_ptr(a.q + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
     const char *db = uniform_ptr(a.dout + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
     Tl::template fill<128, kWaves, false>(vb + (int64_t)K0 * a.v_t, (uint32_t)a.v_t, kend - K0, at_v, wave, lane);
+    // the tile asked for last: 32 queries from t0 + str_row on, of one head
+    int str_row = 0, str_head = 0;
     float row = 0.f;
-    auto load_tile = [&](int it) {
-      const int hd = it % G, r0 = it / G * 32, nv = n_rows - r0;
-      const uint32_t at = at_s + (uint32_t)(it & 1) * (2 * kTileB);
-      const int64_t o = (int64_t)r0 * a.o_t + (int64_t)hd * a.o_h;
-      Tl::template fill<32, kWaves, false>(qb + o, (uint32_t)a.o_t, nv, at, wave, lane);
-      Tl::template fill<32, kWaves, false>(db + o, (uint32_t)a.o_t, nv, at + kTileB, wave, lane);
+    auto load_tile = [&](uint32_t buf) {
+      const int nv = n_rows - str_row;
+      const int64_t o = (int64_t)str_row * a.o_t + (int64_t)str_head * a.o_h;
+      Tl::template fill<32, kWaves, false>(qb + o, (uint32_t)a.o_t, nv, at_s + buf, wave, lane);
+      Tl::template fill<32, kWaves, false>(db + o, (uint32_t)a.o_t, nv, at_s + buf + kTileB, wave, lane);
       if (wave == 0) {   // lse and D of its rows
-        int r = r0 + l32;
+        int r = str_row + l32;
         r = (r < n_rows ? r : n_rows - 1) + t0 - off;
-        row = g == 0 ? lse_log2(a.lse[b * a.l_b + (int64_t)r * a.l_t + (int64_t)(hkv * G + hd) * a.l_h])
-                     : a.delta[((int64_t)b * a.Hq + hkv * G + hd) * a.Tq + r];
+        row = g == 0 ? a.lse[b * a.l_b + (int64_t)r * a.l_t + (int64_t)(hkv * G + str_head) * a.l_h]
+                     : a.delta[((int64_t)b * a.Hq + hkv * G + str_head) * a.Tq + r];
       }
     };
     Operand<T> kf[KS];
@@ -528,52 +580,81 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
     load_row<T, D>(kb + (int64_t)(key < kend ? key : kend - 1) * a.k_t, g, kf);
     const float c = a.scale * kLog2e;
     const int wk0 = K0 + 32 * wave;
-    for (int it = 0; it < n_tiles; ++it) {
-      if (wave == 0) rows[(it & 1) * 64 + lane] = row;
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      if (it + 1 < n_tiles) load_tile(it + 1);
-      const int p0 = t0 + it / G * 32;   // position of the tile's first query
-      if (wk0 >= kend || (!far && (p0 + 31 < wk0 || p0 - (wk0 + 31) >= a.W))) continue;
-      const uint32_t qt = at_s + (uint32_t)(it & 1) * (2 * kTileB), dt = qt + kTileB;
+    const Fragments<T, D> fr(at_s, at_s, lane);
+    const uint32_t v_off = 4 * kTileB + (uint32_t)(32 * wave * Tl::kRowB);   // of the wave's rows of v, from the first q tile on
+    auto tile_step = [&](int it, auto parity) {
+      constexpr uint32_t kBuf = decltype(parity)::value * (2 * kTileB);
+      if (wave == 0) rows[decltype(parity)::value * 64 + lane] = g == 0 ? lse_log2(row) : row;
+      wait_vmem<0>();
+      publish();
+      const int p0 = t0 + str_row;   // position of the tile's first query
+      if (it + 1 < n_tiles) {
+        if (++str_head == G) {
+          str_head = 0;
+          str_row += 32;
+        }
+        load_tile(2 * kTileB - kBuf);
+      }
+      if (wk0 >= kend || (!far && (p0 + 31 < wk0 || p0 - (wk0 + 31) >= a.W))) return;
       const bool masked = far || !(p0 >= wk0 + 31 && p0 + 31 - wk0 < a.W && p0 + 32 <= t1);
       f32x16 s, dp;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = dp[v] = 0.f;
+      for (int ks = 0; ks < KS; ++ks) s = mma(fr.along(0, ks, kBuf), kf[ks], ks == 0 ? f32x16{0.f} : s);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mma(Tl::along(qt + lane_along, 0, ks), kf[ks], s);
+      for (int ks = 0; ks < KS; ++ks) dp = mma(fr.along(0, ks, kBuf + kTileB), fr.along(0, ks, v_off), ks == 0 ? f32x16{0.f} : dp);
+      const float *rl = rows + decltype(parity)::value * 64 + 4 * g;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) dp = mma(Tl::along(dt + lane_along, 0, ks), Tl::along(at_v + (uint32_t)(32 * wave * Tl::kRowB) + lane_along, 0, ks), dp);
-      const float *rl = rows + (it & 1) * 64 + 4 * g;
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const float4 x = *reinterpret_cast<const float4 *>(rl + 8 * v4);
+        const float4 y = *reinterpret_cast<const float4 *>(rl + 32 + 8 * v4);
+        const float lse4[4] = {x.x, x.y, x.z, x.w}, d4[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int v = 4 * v4 + e;
+          s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse4[e]));
+          dp[v] = s[v] * (dp[v] - d4[e]);
+        }
+      }
+      if (masked) {
+        // of the tile's rows, the lane's key is seen by those from `first` to `last`
+        const int first = (far ? key + a.W : key) - p0 - 4 * g;
+        int last = (far ? t1 - 1 : key + a.W - 1) - p0 - 4 * g;
+        const int end = (far && key >= kend ? p0 - 1 : t1 - 1) - p0 - 4 * g;
+        last = last < end ? last : end;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = mfma_row(v, 0);
+          const bool sees = r >= first && r <= last;
+          s[v] = sees ? s[v] : 0.f;
+          dp[v] = sees ? dp[v] : 0.f;
+        }
+      }
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         float p[8], ds[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float4 x = *reinterpret_cast<const float4 *>(rl + 16 * hf + 8 * i);
-          const float4 y = *reinterpret_cast<const float4 *>(rl + 32 + 16 * hf + 8 * i);
-          const float lse4[4] = {x.x, x.y, x.z, x.w}, d4[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = 8 * hf + 4 * i + e, gap = p0 + mfma_row(v, g) - key;
-            bool sees = true;
-            if (masked)
-              sees = p0 + mfma_row(v, g) < t1 && (far ? key < kend && gap >= a.W : gap >= 0 && gap < a.W);
-            const float pr = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse4[e]));
-            p[4 * i + e] = sees ? pr : 0.f;
-            ds[4 * i + e] = sees ? pr * (dp[v] - d4[e]) * a.scale : 0.f;
-          }
+        for (int e = 0; e < 8; ++e) {
+          p[e] = s[8 * hf + e];
+          ds[e] = dp[8 * hf + e];
         }
         Operand<T> pf, sf;
         to_operand(p, pf);
         to_operand(ds, sf);
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
-          dv[i] = mma(Tl::across(dt + lane_across, i, hf), pf, dv[i]);
-          dk[i] = mma(Tl::across(qt + lane_across, i, hf), sf, dk[i]);
+          dv[i] = mma(fr.across(i, hf, kBuf + kTileB), pf, dv[i]);
+          dk[i] = mma(fr.across(i, hf, kBuf), sf, dk[i]);
         }
       }
+    };
+    for (int it = 0; it < n_tiles; it += 2) {
+      tile_step(it, std::integral_constant<uint32_t, 0>{});
+      if (it + 1 < n_tiles) tile_step(it + 1, std::integral_constant<uint32_t, 1>{});
     }
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) dk[i][v] *= a.scale;
   }
   const int parts = a.n_split + 1;
   if (far || (a.n_split > 0 && key < a.S)) {   // a sink's share
@@ -855,11 +936,11 @@ WinArgs base_args(const kvm_window_config *c, int64_t Tq, int64_t Tk, const int3
   a.Tq = (int32_t)Tq; a.Tk = (int32_t)Tk;
   a.W = (int32_t)(c->window < Tk ? c->window : Tk);
   a.S = a.W >= Tk ? 0 : (int32_t)(c->n_sink < Tk ? c->n_sink : Tk);   // (nothing is beyond the window: no sinks needed)
-  const int G = a.Hq / a.Hkv;
-  a.by_head = G % kWaves == 0;
-  a.tiles = (int32_t)((Tq + (a.by_head ? 32 : 128) - 1) / (a.by_head ? 32 : 128));
+  a.by_head = a.Hq / a.Hkv % kWaves == 0;
+  a.span = a.by_head ? 32 : 32 * kWaves;
+  a.tiles = (int32_t)((Tq + a.span - 1) / a.span);
   // blocks of position tiles: 2048 positions, fewer where there would not be eight for every XCD
-  int64_t per = a.by_head ? 64 : 16;
+  int64_t per = 2048 / a.span;
   const int64_t units = (int64_t)a.B * a.Hkv;
   while (per > 1 && units * ((a.tiles + per - 1) / per) < 8 * kXcds) per /= 2;
   a.per_block = (int32_t)per;
@@ -889,7 +970,7 @@ size_t part_bytes(const WinArgs &a, int d) {
 template <typename T, int D>
 hipError_t run_prefill(const WinArgs &a, unsigned grid, hipStream_t st) {
   static OncePerDevice<hipError_t> once;
-  constexpr size_t bytes = 4 * (size_t)kTileRows<T, D> * D * sizeof(T);
+  constexpr size_t bytes = 4 * (size_t)kPromptRows<T, D> * D * sizeof(T);
   hipError_t e = allow_lds(once, (const void *)window_prefill_kernel<T, D>, bytes);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((window_prefill_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);

@@ -6,6 +6,7 @@ torch is used for device memory and the current stream.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -620,6 +621,7 @@ def decode_multi_static(states, q, k, v, gate=None, *, out):
 
 
 # ---- the mixers beside the layer: linear attention with decay, sliding-window attention with sinks
+# (A single token is a few microseconds of GPU work: its calls find their configuration and workspace size by one look-up.)
 
 _IO_OF = {torch.bfloat16: KVM_BF16, torch.float32: KVM_F32}
 
@@ -643,10 +645,10 @@ def _want(t: Optional[torch.Tensor], shape, dtype, device, name: str, rows: bool
     return t.data_ptr()
 
 
-def _heads(q: torch.Tensor, k: torch.Tensor):
-    if q.dim() < 3 or q.dim() != k.dim() or q.shape[-1] != k.shape[-1] or k.shape[-2] == 0 or q.shape[-2] % k.shape[-2]:
-        raise ValueError(f"q and k: query heads have to be a multiple of KV heads of the same size, got {tuple(q.shape)} and "
-                         f"{tuple(k.shape)}")
+def _heads(q: torch.Tensor, k: torch.Tensor, dims: int):
+    if q.dim() != dims or k.dim() != dims or q.shape[-1] != k.shape[-1] or k.shape[-2] == 0 or q.shape[-2] % k.shape[-2]:
+        raise ValueError(f"q and k: want {dims} dimensions and query heads that are a multiple of KV heads of the same size, got "
+                         f"{tuple(q.shape)} and {tuple(k.shape)}")
     return q.shape[-2], k.shape[-2], q.shape[-1]
 
 
@@ -655,9 +657,13 @@ def _row_strides(q, k, v, out, lse=None) -> kvm_strides:
     return kvm_strides(*bth(q), *bth(k), *bth(v), *bth(out), 0, 0, 0, *bth(lse))
 
 
+@functools.lru_cache(maxsize=4096)
+def _linear_config_of(B: int, Hq: int, Hkv: int, d: int, io: int, scale: Optional[float]) -> kvm_linear_config:
+    return kvm_linear_config(B, Hq, Hkv, d, io, 0.0 if scale is None else float(scale))
+
+
 def _linear_config(q, k, scale) -> kvm_linear_config:
-    Hq, Hkv, d = _heads(q, k)
-    return kvm_linear_config(q.shape[0], Hq, Hkv, d, _io_of(q), 0.0 if scale is None else float(scale))
+    return _linear_config_of(q.shape[0], *_heads(q, k, 4), _io_of(q), scale)
 
 
 def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional[float] = None, out=None, state_out=None,
@@ -725,26 +731,41 @@ def linear_backward(q, k, v, log_decay, dout, *, state=None, dstate_out=None, le
 def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, active=None, out=None):
     """kvm_linear_decode: one token per sequence; `state` fp32 [B,Hkv,d,d] is advanced in place.  q [B,Hq,d]; k, v [B,Hkv,d];
     active int32 [B] or None: a sequence whose entry is 0 keeps its state and gets zeros."""
-    lib = load_library()
-    cfg = _linear_config(q, k, scale)
-    B, Hkv, d, dev = q.shape[0], cfg.n_kv_heads, cfg.head_dim, q.device
+    Hq, Hkv, d = _heads(q, k, 3)
+    B, dev, dt = q.shape[0], q.device, q.dtype
+    cfg = _linear_config_of(B, Hq, Hkv, d, _io_of(q), scale)
     if out is None:
-        out = torch.empty_like(q)
-    ptrs = [_want(state, (B, Hkv, d, d), torch.float32, dev, "state"), _want(q, q.shape, q.dtype, dev, "q"),
-            _want(k, (B, Hkv, d), q.dtype, dev, "k"), _want(v, (B, Hkv, d), q.dtype, dev, "v"),
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    ptrs = (_want(state, (B, Hkv, d, d), torch.float32, dev, "state"), _want(q, (B, Hq, d), dt, dev, "q"),
+            _want(k, (B, Hkv, d), dt, dev, "k"), _want(v, (B, Hkv, d), dt, dev, "v"),
             _want(log_decay, (Hkv,), torch.float32, dev, "log_decay"), _want(active, (B,), torch.int32, dev, "active"),
-            _want(out, q.shape, q.dtype, dev, "out")]
-    with _on_device(dev):
-        status = lib.kvm_linear_decode(cfg, *ptrs, _stream())
+            _want(out, (B, Hq, d), dt, dev, "out"))
+    lib = _lib or load_library()
+    if _current_device() == dev.index:
+        status = lib.kvm_linear_decode(cfg, *ptrs, _raw_stream(dev.index))
+    else:
+        with _on_device(dev):
+            status = lib.kvm_linear_decode(cfg, *ptrs, _stream())
     if status != KVM_OK:
         _check(status, "kvm_linear_decode")
     return out
 
 
+@functools.lru_cache(maxsize=4096)
 def _window_config(B: int, Hq: int, Hkv: int, d: int, io: int, window: int, n_sink: int, scale) -> kvm_window_config:
     if not 1 <= int(window) < 1 << 30 or not 0 <= int(n_sink) <= KVM_WINDOW_MAX_SINK:
         raise ValueError(f"window: want 1 .. 2^30 - 1, n_sink 0 .. {KVM_WINDOW_MAX_SINK}, got {window} and {n_sink}")
     return kvm_window_config(B, Hq, Hkv, d, io, int(n_sink), int(window), 0.0 if scale is None else float(scale))
+
+
+@functools.lru_cache(maxsize=4096)
+def _window_token_config(*sizes):
+    """The configuration of a decode step and its workspace's bytes."""
+    cfg = _window_config(*sizes)
+    nbytes = load_library().kvm_window_decode_workspace_bytes(cfg)
+    if nbytes == 0:
+        raise KVMError(KVM_ERR_ARG, "kvm_window_decode_workspace_bytes: unsupported sizes")
+    return cfg, nbytes
 
 
 def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: Optional[float] = None, out=None,
@@ -753,7 +774,7 @@ def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: O
     (bf16 or fp32; views whose head_dim is contiguous), query i at position i + Tk - Tq; lens int32 [B], the sequences' keys in a padded
     batch.  Returns out, or (out, lse [B,Tq,Hq] fp32)."""
     lib = load_library()
-    Hq, Hkv, d = _heads(q, k)
+    Hq, Hkv, d = _heads(q, k, 4)
     B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
     if not 0 < Tq <= Tk:
         raise ValueError(f"q and k: want 0 < Tq <= Tk, got {Tq} and {Tk}")
@@ -777,7 +798,7 @@ def window_backward(q, k, v, out, lse, dout, *, window: int, n_sink: int = 0, le
                     out_rest=None):
     """kvm_window_backward: (dq, dk, dv) of a window_prefill over these tensors (contiguous)."""
     lib = load_library()
-    Hq, Hkv, d = _heads(q, k)
+    Hq, Hkv, d = _heads(q, k, 4)
     B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
     cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
@@ -825,22 +846,22 @@ def window_fill(cache_k, cache_v, k, v, *, window: int, n_sink: int = 0, lens=No
 def window_decode(cache_k, cache_v, q, k, v, pos, *, window: int, n_sink: int = 0, scale: Optional[float] = None, out=None):
     """kvm_window_decode: one token per sequence, at positions pos (int32 [B]; below 0: no token, zeros), stored into the cache and
     attended.  q [B,Hq,d]; k, v [B,Hkv,d]."""
-    lib = load_library()
-    Hq, Hkv, d = _heads(q, k)
-    B, dev = q.shape[0], q.device
-    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
+    Hq, Hkv, d = _heads(q, k, 3)
+    B, dev, dt = q.shape[0], q.device, q.dtype
+    cfg, nbytes = _window_token_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
     if out is None:
-        out = torch.empty_like(q)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     rows = (B, Hkv, n_sink + window, d)
-    ptrs = [_want(cache_k, rows, q.dtype, dev, "cache_k"), _want(cache_v, rows, q.dtype, dev, "cache_v"),
-            _want(q, q.shape, q.dtype, dev, "q"), _want(k, (B, Hkv, d), q.dtype, dev, "k"), _want(v, (B, Hkv, d), q.dtype, dev, "v"),
-            _want(pos, (B,), torch.int32, dev, "pos"), _want(out, q.shape, q.dtype, dev, "out")]
-    nbytes = lib.kvm_window_decode_workspace_bytes(cfg)
-    if nbytes == 0:
-        raise KVMError(KVM_ERR_ARG, "kvm_window_decode_workspace_bytes: unsupported sizes")
+    ptrs = (_want(cache_k, rows, dt, dev, "cache_k"), _want(cache_v, rows, dt, dev, "cache_v"),
+            _want(q, (B, Hq, d), dt, dev, "q"), _want(k, (B, Hkv, d), dt, dev, "k"), _want(v, (B, Hkv, d), dt, dev, "v"),
+            _want(pos, (B,), torch.int32, dev, "pos"), _want(out, (B, Hq, d), dt, dev, "out"))
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    with _on_device(dev):
-        status = lib.kvm_window_decode(cfg, *ptrs, ws.data_ptr(), nbytes, _stream())
+    lib = _lib or load_library()
+    if _current_device() == dev.index:
+        status = lib.kvm_window_decode(cfg, *ptrs, ws.data_ptr(), nbytes, _raw_stream(dev.index))
+    else:
+        with _on_device(dev):
+            status = lib.kvm_window_decode(cfg, *ptrs, ws.data_ptr(), nbytes, _stream())
     if status != KVM_OK:
         _check(status, "kvm_window_decode")
     return out

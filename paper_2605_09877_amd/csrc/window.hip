@@ -37,8 +37,9 @@ struct WinArgs {
   const char *dout;
   char *dq, *dk, *dv;
   float *delta;    // [B, Hq, Tq]
-  float *part;     // [units, n_split + 1, 2, 128 (S rounded up to 32 used), D]
+  float *part;     // [units, parts, 2, sink_rows, D]: shares of the sinks' dk and dv, the last from the queries of their window
   int32_t n_split, split_q;   // ranges that the queries beyond a sink's window are cut into, and their length
+  int32_t sink_rows, parts;   // S up to 32, 64 or 128; shares
   int32_t key_tiles;
 };
 
@@ -503,42 +504,39 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
 }
 
 // dk and dv of 128 keys, 32 to a wave (K in registers, V in LDS); the queries that see them, head after head of the group, stream
-// in tiles of 32.  Sinks (keys below S) are also seen by every query beyond their window: those are cut into n_split ranges with a workgroup
-// each, and what ranges and window give for sinks is added up by window_sinks_kernel.
+// in tiles of 32.  Sinks (keys below S) are also seen by every query beyond their window: by a launch of its own (far), which cuts
+// those into n_split ranges, a workgroup each; its waves share the range's tiles among them (or the sinks, 32 to a wave), each with
+// tiles of its own and no barrier.  What ranges and window give for sinks is added up by window_sinks_kernel.
 template <typename T, int D>
 constexpr size_t kv_lds() {
-  return (4 * 32 + 128) * (size_t)D * sizeof(T) + 2 * 64 * sizeof(float);
+  return (4 * 32 + 128) * (size_t)D * sizeof(T) + 4 * 64 * sizeof(float);
 }
-template <typename T, int D>
+template <typename T, int D, bool far>
 __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_kernel(WinArgs a) {
   using Tl = Tile<T, D>;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = 32 * Tl::kRowB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t at_s = lds_addr_of(lds), at_v = at_s + 4 * kTileB;   // stage: q tile, dout tile; then 128 rows of v
-  float *rows = reinterpret_cast<float *>(lds + 8 * kTileB);           // [stage][lse, in powers of two | D][32]
+  float *rows = reinterpret_cast<float *>(lds + 8 * kTileB);           // [stage or wave][lse, in powers of two | D][32]
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, l32 = lane & 31;
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq, units = a.B * a.Hkv;
-  const int per_unit = a.key_tiles + a.n_split;
   // a unit's workgroups go to one XCD
-  const int xcd = blockIdx.x % kXcds, seq = blockIdx.x / kXcds;
-  const int u = seq / per_unit * kXcds + xcd;
-  int member = seq % per_unit;
+  const int per_unit = far ? a.n_split : a.key_tiles;
+  const int u = blockIdx.x / kXcds / per_unit * kXcds + blockIdx.x % kXcds, member = blockIdx.x / kXcds % per_unit;
   if (u >= units) return;
-  const bool far = member < a.n_split;   // queries beyond the sinks' window (longest: first)
-  const int split = member;
-  if (!far) member -= a.n_split;
   const int b = u / a.Hkv, hkv = u % a.Hkv;
   const int n = tokens_of(a, b);
+  const int n_kb = a.sink_rows / 32, tw = wave / n_kb;   // far: blocks of sinks, the wave's part of the tiles
   const int K0 = far ? 0 : 128 * member;
   const int kend = far ? (a.S < n ? a.S : n) : (K0 + 128 < n ? K0 + 128 : n);
-  const int key = K0 + 32 * wave + l32;
+  const int wk0 = K0 + 32 * (far ? wave % n_kb : wave), key = wk0 + l32;
   // positions of the queries streamed
   int t0, t1;
   if (far) {
-    t0 = a.W + split * a.split_q;
+    t0 = a.W + member * a.split_q;
     t1 = t0 + a.split_q;
   } else {
     t0 = K0;
@@ -559,54 +557,24 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
     const char *vb = uniform_ptr(a.v + b * a.v_b + (int64_t)hkv * a.v_h);
     const char *qb = uniform_ptr(a.q + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
     const char *db = uniform_ptr(a.dout + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
-    Tl::template fill<128, kWaves, false>(vb + (int64_t)K0 * a.v_t, (uint32_t)a.v_t, kend - K0, at_v, wave, lane);
     // the tile asked for last: 32 queries from t0 + str_row on, of one head
     int str_row = 0, str_head = 0;
-    float row = 0.f;
-    auto load_tile = [&](uint32_t buf) {
-      const int nv = n_rows - str_row;
-      const int64_t o = (int64_t)str_row * a.o_t + (int64_t)str_head * a.o_h;
-      Tl::template fill<32, kWaves, false>(qb + o, (uint32_t)a.o_t, nv, at_s + buf, wave, lane);
-      Tl::template fill<32, kWaves, false>(db + o, (uint32_t)a.o_t, nv, at_s + buf + kTileB, wave, lane);
-      if (wave == 0) {   // lse and D of its rows
-        int r = str_row + l32;
-        r = (r < n_rows ? r : n_rows - 1) + t0 - off;
-        row = g == 0 ? a.lse[b * a.l_b + (int64_t)r * a.l_t + (int64_t)(hkv * G + str_head) * a.l_h]
-                     : a.delta[((int64_t)b * a.Hq + hkv * G + str_head) * a.Tq + r];
-      }
+    // lse (the lower half of the wave) or D of its rows
+    auto row_value = [&]() {
+      int r = str_row + l32;
+      r = (r < n_rows ? r : n_rows - 1) + t0 - off;
+      return g == 0 ? a.lse[b * a.l_b + (int64_t)r * a.l_t + (int64_t)(hkv * G + str_head) * a.l_h]
+                    : a.delta[((int64_t)b * a.Hq + hkv * G + str_head) * a.Tq + r];
     };
-    Operand<T> kf[KS];
-    load_tile(0);
-    load_row<T, D>(kb + (int64_t)(key < kend ? key : kend - 1) * a.k_t, g, kf);
     const float c = a.scale * kLog2e;
-    const int wk0 = K0 + 32 * wave;
-    const Fragments<T, D> fr(at_s, at_s, lane);
-    const uint32_t v_off = 4 * kTileB + (uint32_t)(32 * wave * Tl::kRowB);   // of the wave's rows of v, from the first q tile on
-    auto tile_step = [&](int it, auto parity) {
-      constexpr uint32_t kBuf = decltype(parity)::value * (2 * kTileB);
-      if (wave == 0) rows[decltype(parity)::value * 64 + lane] = g == 0 ? lse_log2(row) : row;
-      wait_vmem<0>();
-      publish();
-      const int p0 = t0 + str_row;   // position of the tile's first query
-      if (it + 1 < n_tiles) {
-        if (++str_head == G) {
-          str_head = 0;
-          str_row += 32;
-        }
-        load_tile(2 * kTileB - kBuf);
-      }
-      if (wk0 >= kend || (!far && (p0 + 31 < wk0 || p0 - (wk0 + 31) >= a.W))) return;
-      const bool masked = far || !(p0 >= wk0 + 31 && p0 + 31 - wk0 < a.W && p0 + 32 <= t1);
-      f32x16 s, dp;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mma(fr.along(0, ks, kBuf), kf[ks], ks == 0 ? f32x16{0.f} : s);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) dp = mma(fr.along(0, ks, kBuf + kTileB), fr.along(0, ks, v_off), ks == 0 ? f32x16{0.f} : dp);
-      const float *rl = rows + decltype(parity)::value * 64 + 4 * g;
+    Operand<T> kf[KS];
+    load_row<T, D>(kb + (int64_t)(key < kend ? key : kend - 1) * a.k_t, g, kf);
+    // P and dS of a tile whose logits are in s and dP in dp, lse and D of its rows at rl
+    auto weights = [&](f32x16 &s, f32x16 &dp, const float *rl) {
 #pragma unroll
       for (int v4 = 0; v4 < 4; ++v4) {
-        const float4 x = *reinterpret_cast<const float4 *>(rl + 8 * v4);
-        const float4 y = *reinterpret_cast<const float4 *>(rl + 32 + 8 * v4);
+        const float4 x = *reinterpret_cast<const float4 *>(rl + 4 * g + 8 * v4);
+        const float4 y = *reinterpret_cast<const float4 *>(rl + 4 * g + 32 + 8 * v4);
         const float lse4[4] = {x.x, x.y, x.z, x.w}, d4[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -615,20 +583,19 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
           dp[v] = s[v] * (dp[v] - d4[e]);
         }
       }
-      if (masked) {
-        // of the tile's rows, the lane's key is seen by those from `first` to `last`
-        const int first = (far ? key + a.W : key) - p0 - 4 * g;
-        int last = (far ? t1 - 1 : key + a.W - 1) - p0 - 4 * g;
-        const int end = (far && key >= kend ? p0 - 1 : t1 - 1) - p0 - 4 * g;
-        last = last < end ? last : end;
+    };
+    // rows first .. last of the tile see the lane's key
+    auto mask = [&](f32x16 &s, f32x16 &dp, int first, int last) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int r = mfma_row(v, 0);
-          const bool sees = r >= first && r <= last;
-          s[v] = sees ? s[v] : 0.f;
-          dp[v] = sees ? dp[v] : 0.f;
-        }
+      for (int v = 0; v < 16; ++v) {
+        const int r = mfma_row(v, 0) + 4 * g;
+        const bool sees = r >= first && r <= last;
+        s[v] = sees ? s[v] : 0.f;
+        dp[v] = sees ? dp[v] : 0.f;
       }
+    };
+    // dv += dout^T P, dk += q^T dS
+    auto add_up = [&](const f32x16 &s, const f32x16 &dp, const Fragments<T, D> &fr, uint32_t buf) {
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         float p[8], ds[8];
@@ -642,25 +609,94 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
         to_operand(ds, sf);
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
-          dv[i] = mma(fr.across(i, hf, kBuf + kTileB), pf, dv[i]);
-          dk[i] = mma(fr.across(i, hf, kBuf), sf, dk[i]);
+          dv[i] = mma(fr.across(i, hf, buf + kTileB), pf, dv[i]);
+          dk[i] = mma(fr.across(i, hf, buf), sf, dk[i]);
         }
       }
     };
-    for (int it = 0; it < n_tiles; it += 2) {
-      tile_step(it, std::integral_constant<uint32_t, 0>{});
-      if (it + 1 < n_tiles) tile_step(it + 1, std::integral_constant<uint32_t, 1>{});
+    if constexpr (far) {
+      const int step = kWaves / n_kb;   // tiles of this wave: tw, tw + step, ..
+      const uint32_t at = at_s + (uint32_t)wave * (2 * kTileB);
+      const Fragments<T, D> fr(at, at, lane);
+      Operand<T> vf[KS];
+      load_row<T, D>(vb + (int64_t)(key < kend ? key : kend - 1) * a.v_t, g, vf);
+      for (int it = tw; it < n_tiles; it += step) {
+        str_head = it % G;
+        str_row = it / G * 32;
+        const int64_t o = (int64_t)str_row * a.o_t + (int64_t)str_head * a.o_h;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile before has been read
+        Tl::template fill<32, 1, false>(qb + o, (uint32_t)a.o_t, n_rows - str_row, at, 0, lane);
+        Tl::template fill<32, 1, false>(db + o, (uint32_t)a.o_t, n_rows - str_row, at + kTileB, 0, lane);
+        const float row = row_value();
+        rows[wave * 64 + lane] = g == 0 ? lse_log2(row) : row;
+        wait_vmem<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        f32x16 s, dp;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mma(fr.along(0, ks, 0), kf[ks], ks == 0 ? f32x16{0.f} : s);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mma(fr.along(0, ks, kTileB), vf[ks], ks == 0 ? f32x16{0.f} : dp);
+        weights(s, dp, rows + wave * 64);
+        const int p0 = t0 + str_row;
+        mask(s, dp, key + a.W - p0, key < kend ? t1 - 1 - p0 : -1);
+        add_up(s, dp, fr, 0);
+      }
+    } else {
+      float row = 0.f;
+      auto load_tile = [&](uint32_t buf) {
+        const int nv = n_rows - str_row;
+        const int64_t o = (int64_t)str_row * a.o_t + (int64_t)str_head * a.o_h;
+        Tl::template fill<32, kWaves, false>(qb + o, (uint32_t)a.o_t, nv, at_s + buf, wave, lane);
+        Tl::template fill<32, kWaves, false>(db + o, (uint32_t)a.o_t, nv, at_s + buf + kTileB, wave, lane);
+        if (wave == 0) row = row_value();
+      };
+      load_tile(0);
+      Tl::template fill<128, kWaves, false>(vb + (int64_t)K0 * a.v_t, (uint32_t)a.v_t, kend - K0, at_v, wave, lane);
+      const Fragments<T, D> fr(at_s, at_s, lane);
+      const uint32_t at_rows = at_v + (uint32_t)(32 * wave * Tl::kRowB) + Tl::along0(lane);   // of the wave's rows of v
+      auto tile_step = [&](int it, auto parity) {
+        constexpr uint32_t kBuf = decltype(parity)::value * (2 * kTileB);
+        if (wave == 0) rows[decltype(parity)::value * 64 + lane] = g == 0 ? lse_log2(row) : row;
+        wait_vmem<0>();
+        publish();
+        const int p0 = t0 + str_row;   // position of the tile's first query
+        if (it + 1 < n_tiles) {
+          if (++str_head == G) {
+            str_head = 0;
+            str_row += 32;
+          }
+          load_tile(2 * kTileB - kBuf);
+        }
+        if (wk0 >= kend || p0 + 31 < wk0 || p0 - (wk0 + 31) >= a.W) return;
+        const uint32_t v0 = here(at_rows);
+        // (ahead of the other workgroup's wave while this one feeds the matrix cores: 752 us of the 2 x 8k shape, 708 with it)
+        __builtin_amdgcn_s_setprio(1);
+        f32x16 s, dp;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mma(fr.along(0, ks, kBuf), kf[ks], ks == 0 ? f32x16{0.f} : s);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mma(fr.along(0, ks, kBuf + kTileB), Tl::along(v0, 0, ks), ks == 0 ? f32x16{0.f} : dp);
+        __builtin_amdgcn_s_setprio(0);
+        weights(s, dp, rows + decltype(parity)::value * 64);
+        if (!(p0 >= wk0 + 31 && p0 + 31 - wk0 < a.W && p0 + 32 <= t1))
+          mask(s, dp, key - p0, (key + a.W < t1 ? key + a.W : t1) - 1 - p0);
+        add_up(s, dp, fr, kBuf);
+      };
+      for (int it = 0; it < n_tiles; it += 2) {
+        tile_step(it, std::integral_constant<uint32_t, 0>{});
+        if (it + 1 < n_tiles) tile_step(it + 1, std::integral_constant<uint32_t, 1>{});
+      }
     }
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
       for (int v = 0; v < 16; ++v) dk[i][v] *= a.scale;
   }
-  const int parts = a.n_split + 1;
-  if (far || (a.n_split > 0 && key < a.S)) {   // a sink's share
+  if (far || key < a.S) {   // a sink's share
     if (key < a.S) {
-      float *pk = a.part + ((((int64_t)u * parts + (far ? split : a.n_split)) * 2) * kMaxSink + key) * D;
-      float *pv = pk + kMaxSink * D;
+      const int share = far ? member * (kWaves / n_kb) + tw : a.parts - 1;
+      float *pk = a.part + ((((int64_t)u * a.parts + share) * 2) * a.sink_rows + key) * D;
+      float *pv = pk + (int64_t)a.sink_rows * D;
 #pragma unroll
       for (int i = 0; i < 4 * DB; ++i)
 #pragma unroll
@@ -691,18 +727,21 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
   }
 }
 
-// dk and dv of the sinks: the sum of their shares, in order.
+// dk and dv of the sinks: the sums of their shares, four of them for every value, and these added.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_sinks_kernel(WinArgs a) {
-  const int u = blockIdx.y, b = u / a.Hkv, hkv = u % a.Hkv, parts = a.n_split + 1;
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= 2 * a.S * D) return;
+  __shared__ float sums[4][64];
+  const int u = blockIdx.y, b = u / a.Hkv, hkv = u % a.Hkv, quarter = threadIdx.x / 64;
+  const int i = blockIdx.x * 64 + threadIdx.x % 64;   // (2 S D is a multiple of 64)
   const int which = i / (a.S * D), key = i / D % a.S, ch = i % D;
-  if (key >= a.Tk) return;
-  const float *p = a.part + (((int64_t)u * parts * 2 + which) * kMaxSink + key) * D + ch;
+  const float *p = a.part + (((int64_t)u * a.parts * 2 + which) * a.sink_rows + key) * D + ch;
   float sum = 0.f;
-  for (int s = 0; s < parts; ++s) sum += p[(int64_t)s * 2 * kMaxSink * D];
-  if (key >= tokens_of(a, b)) sum = 0.f;
+#pragma unroll 4
+  for (int s = quarter; s < a.parts; s += 4) sum += p[(int64_t)s * 2 * a.sink_rows * D];
+  sums[quarter][threadIdx.x % 64] = sum;
+  __syncthreads();
+  if (quarter != 0 || key >= a.Tk) return;
+  sum = key < tokens_of(a, b) ? (sum + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]) : 0.f;
   char *dst = which ? a.dv + b * a.v_b + (int64_t)key * a.v_t + (int64_t)hkv * a.v_h
                     : a.dk + b * a.k_b + (int64_t)key * a.k_t + (int64_t)hkv * a.k_h;
   Io<T>::store((T *)dst + ch, sum);
@@ -753,8 +792,8 @@ __global__ __launch_bounds__(256) void window_token_kernel(CacheArgs a) {
   const int split = blockIdx.x % a.n_split, bu = blockIdx.x / a.n_split;
   const int u = bu / batches, g0 = bu % batches * kHeads, b = u / a.Hkv;
   const int ng = G - g0 < kHeads ? G - g0 : kHeads;
-  const int64_t rows = a.S + a.W;
-  const int64_t pos = a.at[b];
+  const uint32_t rows = (uint32_t)a.S + (uint32_t)a.W;
+  const int pos = a.at[b];
   const int c = lane % kLanes, sub = wave * kRowsWave + lane / kLanes;
   const int64_t head0 = (int64_t)u * G + g0;   // of [B, Hq]
   float *po = a.n_split > 1 ? a.part + (head0 * a.n_split + split) * (D + 2) : nullptr;
@@ -763,15 +802,15 @@ __global__ __launch_bounds__(256) void window_token_kernel(CacheArgs a) {
       for (int i = tid; i < ng * D; i += 256) Io<T>::store((T *)a.out + head0 * D + i, 0.f);
     return;
   }
-  const int64_t fresh = pos < a.S ? pos : a.S + (pos - a.S) % a.W;   // the token's own row
-  const int64_t r0 = (int64_t)split * a.split_rows;
-  int64_t r1 = r0 + a.split_rows < rows ? r0 + a.split_rows : rows;
-  r1 = r1 <= pos ? r1 : pos + 1;   // rows that hold a token
-  const char *ck = a.ck + (int64_t)u * rows * D * sizeof(T), *cv = a.cv + (int64_t)u * rows * D * sizeof(T);
+  const uint32_t fresh = pos < a.S ? (uint32_t)pos : (uint32_t)a.S + (uint32_t)(pos - a.S) % (uint32_t)a.W;   // the token's own row
+  const uint32_t r0 = (uint32_t)split * (uint32_t)a.split_rows;
+  uint32_t r1 = r0 + (uint32_t)a.split_rows < rows ? r0 + (uint32_t)a.split_rows : rows;
+  r1 = r1 <= (uint32_t)pos ? r1 : (uint32_t)pos + 1;   // rows that hold a token
+  const char *ck = a.ck + (int64_t)u * rows * (D * sizeof(T)), *cv = a.cv + (int64_t)u * rows * (D * sizeof(T));
   const char *nk = a.k + (int64_t)u * D * sizeof(T), *nv = a.v + (int64_t)u * D * sizeof(T);
   if (g0 == 0 && fresh >= r0 && fresh < r1 && tid < kLanes) {
-    reinterpret_cast<uint4 *>(a.ck + ((int64_t)u * rows + fresh) * D * sizeof(T))[tid] = reinterpret_cast<const uint4 *>(nk)[tid];
-    reinterpret_cast<uint4 *>(a.cv + ((int64_t)u * rows + fresh) * D * sizeof(T))[tid] = reinterpret_cast<const uint4 *>(nv)[tid];
+    reinterpret_cast<uint4 *>(a.ck + ((int64_t)u * rows + fresh) * (D * sizeof(T)))[tid] = reinterpret_cast<const uint4 *>(nk)[tid];
+    reinterpret_cast<uint4 *>(a.cv + ((int64_t)u * rows + fresh) * (D * sizeof(T)))[tid] = reinterpret_cast<const uint4 *>(nv)[tid];
   }
   float q[kHeads][kVec], o[kHeads][kVec], m[kHeads], l[kHeads];
   const float sc = a.scale * kLog2e;
@@ -786,14 +825,14 @@ __global__ __launch_bounds__(256) void window_token_kernel(CacheArgs a) {
     m[h] = -INFINITY;
     l[h] = 0.f;
   }
-  for (int64_t r = r0 + sub; r < r1; r += kRowsWg * kUnroll) {
+  for (uint32_t r = r0 + (uint32_t)sub; r < r1; r += kRowsWg * kUnroll) {
     uint4 kx[kUnroll], vx[kUnroll];
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
-      int64_t ri = r + i * kRowsWg;
+      uint32_t ri = r + i * kRowsWg;
       ri = ri < r1 ? ri : r;
-      kx[i] = reinterpret_cast<const uint4 *>(ri == fresh ? nk : ck + ri * D * sizeof(T))[c];
-      vx[i] = reinterpret_cast<const uint4 *>(ri == fresh ? nv : cv + ri * D * sizeof(T))[c];
+      kx[i] = reinterpret_cast<const uint4 *>(ri == fresh ? nk : ck + (uint64_t)ri * (D * sizeof(T)))[c];
+      vx[i] = reinterpret_cast<const uint4 *>(ri == fresh ? nv : cv + (uint64_t)ri * (D * sizeof(T)))[c];
     }
     float s[kHeads][kUnroll];
 #pragma unroll
@@ -889,22 +928,34 @@ __global__ __launch_bounds__(256) void window_token_kernel(CacheArgs a) {
   }
 }
 
+// The ranges of a query head joined: a lane has a range's maximum and sum, a thread a channel of every kParts-th range.
+constexpr int kMostSplits = 64;
 template <typename T, int D>
-__global__ __launch_bounds__(D) void window_join_kernel(CacheArgs a) {
-  const int64_t head = blockIdx.x;
+__global__ __launch_bounds__(256) void window_join_kernel(CacheArgs a) {
+  constexpr int kParts = 256 / D;
+  __shared__ float factor[kMostSplits], acc[kParts][D];
+  const int head = blockIdx.x, lane = threadIdx.x & 63;
   if (a.at[head / a.Hq] < 0) return;
-  const float *p = a.part + head * a.n_split * (D + 2);
-  float top = -INFINITY;
-  for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, p[s * (D + 2) + D]);
-  float sum = 0.f, x = 0.f;
-  for (int s = 0; s < a.n_split; ++s) {
-    const float ms = p[s * (D + 2) + D], f = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - top);
-    if (f != 0.f) {
-      sum = fmaf(f, p[s * (D + 2) + D + 1], sum);
-      x = fmaf(f, p[s * (D + 2) + threadIdx.x], x);
-    }
+  const float *p = a.part + (int64_t)head * a.n_split * (D + 2);
+  const int ch = threadIdx.x % D, part = threadIdx.x / D;
+  const float *own = p + (lane < a.n_split ? lane : 0) * (D + 2) + D;
+  const float m = lane < a.n_split ? own[0] : -INFINITY, l = own[1];
+  const float top = wave_max(m), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+  const float sum = wave_sum(f == 0.f ? 0.f : f * l);
+  if (threadIdx.x < 64) factor[lane] = f;
+  __syncthreads();
+  float x = 0.f;
+#pragma unroll 8
+  for (int s = part; s < a.n_split; s += kParts) {
+    const float y = p[s * (D + 2) + ch];
+    x = factor[s] == 0.f ? x : fmaf(factor[s], y, x);
   }
-  Io<T>::store((T *)a.out + head * D + threadIdx.x, sum == 0.f ? 0.f : x / sum);
+  acc[part][ch] = x;
+  __syncthreads();
+  if (part != 0) return;
+#pragma unroll
+  for (int k = 1; k < kParts; ++k) x += acc[k][ch];
+  Io<T>::store((T *)a.out + (int64_t)head * D + ch, sum == 0.f ? 0.f : x / sum);
 }
 
 // ---- host side
@@ -953,18 +1004,22 @@ unsigned query_grid(const WinArgs &a) {
   const int64_t n = groups * a.per_block * (a.by_head ? G / kWaves : G);
   return n < (1ll << 31) ? (unsigned)n : 0;
 }
-// The queries beyond a sink's window: ranges so that the far workgroups stream no more than twice what the others do.
+// The queries beyond a sink's window: ranges of one tile of each head for every wave at least, as many as fill the device (two
+// workgroups to a compute unit) and 64 at most.
 void cut_far(WinArgs &a) {
   a.key_tiles = (a.Tk + 127) / 128;
+  a.sink_rows = 32;
   if (a.S == 0) return;
-  const int far = a.Tk - a.W;
-  a.split_q = (a.W + 127 + 31) / 32 * 32;
-  if (a.split_q > 1024) a.split_q = 1024;
+  a.sink_rows = a.S <= 32 ? 32 : a.S <= 64 ? 64 : 128;
+  const int step = kWaves / (a.sink_rows / 32), far = a.Tk - a.W;
+  const int64_t units = (int64_t)a.B * a.Hkv, most = units < 8 ? 64 : units < 512 ? 512 / units : 1;
+  a.split_q = (int32_t)((far + most - 1) / most + 32 * step - 1) / (32 * step) * (32 * step);
   a.n_split = (far + a.split_q - 1) / a.split_q;
+  a.parts = a.n_split * step + 1;
 }
 size_t delta_bytes(const WinArgs &a) { return ((size_t)a.B * a.Hq * a.Tq * sizeof(float) + 255) & ~(size_t)255; }
 size_t part_bytes(const WinArgs &a, int d) {
-  return a.n_split ? (size_t)a.B * a.Hkv * (a.n_split + 1) * 2 * kMaxSink * d * sizeof(float) : 0;
+  return (size_t)a.B * a.Hkv * a.parts * 2 * a.sink_rows * d * sizeof(float);
 }
 
 template <typename T, int D>
@@ -977,30 +1032,35 @@ hipError_t run_prefill(const WinArgs &a, unsigned grid, hipStream_t st) {
   return hipGetLastError();
 }
 template <typename T, int D>
-hipError_t run_backward_as(const WinArgs &a, unsigned grid, unsigned grid_kv, hipStream_t st) {
-  static OncePerDevice<hipError_t> once_q, once_kv;
+hipError_t run_backward_as(const WinArgs &a, unsigned grid, unsigned units8, hipStream_t st) {
+  static OncePerDevice<hipError_t> once_q, once_kv, once_far;
   constexpr size_t bytes = 4 * (size_t)kTileRows<T, D> * D * sizeof(T), bytes_kv = kv_lds<T, D>();
   hipError_t e = allow_lds(once_q, (const void *)window_dq_kernel<T, D>, bytes);
-  if (e == hipSuccess) e = allow_lds(once_kv, (const void *)window_dkv_kernel<T, D>, bytes_kv);
+  if (e == hipSuccess) e = allow_lds(once_kv, (const void *)window_dkv_kernel<T, D, false>, bytes_kv);
+  if (e == hipSuccess && a.n_split > 0) e = allow_lds(once_far, (const void *)window_dkv_kernel<T, D, true>, bytes_kv);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D>), dim3(grid_kv), dim3(256), bytes_kv, st, a);
+  hipLaunchKernelGGL((window_dkv_kernel<T, D, false>), dim3(units8 * a.key_tiles), dim3(256), bytes_kv, st, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.n_split == 0) return e;
-  hipLaunchKernelGGL((window_sinks_kernel<T, D>), dim3((unsigned)((2 * a.S * D + 255) / 256), (unsigned)(a.B * a.Hkv)), dim3(256), 0,
+  hipLaunchKernelGGL((window_dkv_kernel<T, D, true>), dim3(units8 * a.n_split), dim3(256), bytes_kv, st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((window_sinks_kernel<T, D>), dim3((unsigned)(2 * a.S * D / 64), (unsigned)(a.B * a.Hkv)), dim3(256), 0,
                      st, a);
   return hipGetLastError();
 }
 
+constexpr int64_t kTokenWgs = 4096;
 // Ranges a unit's cache rows are cut into: workgroups enough to fill the device, 64 rows at least in each.
 void cut_rows(CacheArgs &a, const kvm_window_config *c) {
   const int64_t rows = c->n_sink + c->window, G = c->n_q_heads / c->n_kv_heads;
   const int64_t wgs = (int64_t)c->batch * c->n_kv_heads * ((G + kHeads - 1) / kHeads);
-  int64_t n = (1024 + wgs - 1) / wgs, most = (rows + 63) / 64;
+  int64_t n = (kTokenWgs + wgs - 1) / wgs, most = (rows + 63) / 64;
   if (n > most) n = most;
-  if (n > 64) n = 64;
+  if (n > kMostSplits) n = kMostSplits;
   const int64_t per = ((rows + n - 1) / n + 15) / 16 * 16;
   a.split_rows = (int32_t)per;
   a.n_split = (int32_t)((rows + per - 1) / per);
@@ -1010,7 +1070,7 @@ hipError_t run_token(const CacheArgs &a, unsigned grid, hipStream_t st) {
   hipLaunchKernelGGL((window_token_kernel<T, D>), dim3(grid), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)(a.B * a.Hq)), dim3(D), 0, st, a);
+  hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -1086,9 +1146,9 @@ extern "C" int kvm_window_backward(const kvm_window_config *cfg, const void *q, 
   a.delta = (float *)workspace;
   a.part = (float *)((char *)workspace + delta_bytes(a));
   const unsigned grid = query_grid(a);
-  const int64_t kv = ((int64_t)a.B * a.Hkv + kXcds - 1) / kXcds * kXcds * (a.key_tiles + a.n_split);
-  if (grid == 0 || kv >= (1ll << 31) || (int64_t)a.B * a.Hkv > 65535) return KVM_ERR_ARG;
-  const hipError_t e = KVM_BY_TYPE(cfg, run_backward_as, a, grid, (unsigned)kv, (hipStream_t)stream);
+  const int64_t units8 = ((int64_t)a.B * a.Hkv + kXcds - 1) / kXcds * kXcds;
+  if (grid == 0 || units8 * a.key_tiles >= (1ll << 31) || (int64_t)a.B * a.Hkv > 65535) return KVM_ERR_ARG;
+  const hipError_t e = KVM_BY_TYPE(cfg, run_backward_as, a, grid, (unsigned)units8, (hipStream_t)stream);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_backward");
 }
 

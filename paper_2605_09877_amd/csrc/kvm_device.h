@@ -152,6 +152,29 @@ __device__ __forceinline__ V group_sum(V x) {
   return x;
 }
 
+// Sum and maximum over the 64 / kLanes lanes that are kLanes apart, in every one of them.
+template <bool k32>
+__device__ __forceinline__ float swap_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = k32 ? __builtin_amdgcn_permlane32_swap(u, u, false, false)
+                     : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <int kLanes>
+__device__ __forceinline__ float strided_sum(float x) {
+  static_assert(kLanes == 8 || kLanes == 16 || kLanes == 32, "stride");
+  if (kLanes <= 8) x += dpp_get<0x128>(x);   // row_ror:8
+  if (kLanes <= 16) x = swap_sum<false>(x);
+  return swap_sum<true>(x);
+}
+template <int kLanes>
+__device__ __forceinline__ float strided_max(float x) {
+  static_assert(kLanes == 8 || kLanes == 16 || kLanes == 32, "stride");
+  if (kLanes <= 8) x = fmaxf(x, dpp_get<0x128>(x));
+  if (kLanes <= 16) x = swap_max<false>(x);
+  return swap_max<true>(x);
+}
+
 template <typename V>
 __device__ __forceinline__ V wave_sum(V x) {
   return group_sum<64>(x);

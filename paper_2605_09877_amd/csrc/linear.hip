@@ -446,9 +446,7 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinTokenArgs a) {
         o[3] = fmaf(x, s[r].w, o[3]);
       }
 #pragma unroll
-      for (int off = kLanes; off < 64; off *= 2)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, kWave);
+      for (int e = 0; e < 4; ++e) o[e] = strided_sum<kLanes>(o[e]);
       if (lane < kLanes)
 #pragma unroll
         for (int e = 0; e < 4; ++e) part[hd][wave][4 * lane + e] = o[e];

@@ -30,16 +30,19 @@ namespace {
 struct LinArgs {
   const char *x, *y, *z;
   char *out;
+  const char *x2;        // a pair's second walk: its x and out (strides of the first's)
+  char *out2;
   int64_t x_b, x_t, x_h, y_b, y_t, y_h, z_b, z_t, z_h, o_b, o_t, o_h;   // bytes
   const float *log_decay;
   const int32_t *lens;   // nullable
   const float *start;    // nullable: the state before the first token walked
-  float *seg;            // [units, n_seg, D, D]: start states of the segments (what each adds to the state, after the first pass)
+  float *seg;            // [units, seg_of_unit, D, D]: start states of segments (what each adds to the state, after the first pass);
+                         // a walk's segment is seg_step of them
   float *end;            // nullable: the state behind the last token walked
   float start_scale, end_scale, scale;
   int32_t transposed;    // start and seg are [z channel][y channel]
   int32_t fine_state;    // the state is a result
-  int32_t T, H, G, units, n_seg, seg_tokens;
+  int32_t T, H, G, units, n_seg, seg_tokens, seg_of_unit, seg_step;
 };
 
 template <typename T>
@@ -50,20 +53,22 @@ template <typename T>
 constexpr int kBlocks = kChunk<T> == 64 ? 3 : 1;
 
 // Two y tiles, z, x; pairs of a chunk as operands (bf16); the powers of the decay.
-template <typename T, int D, bool kFine>
+template <typename T, int D, bool kPair, bool kFine>
 constexpr size_t linear_lds() {
-  return 4 * (size_t)kChunk<T> * D * sizeof(T) + (sizeof(T) == 2 ? kBlocks<T> * (kFine ? 4096 : 2048) : 0) +
-         (32 + 2 * kChunk<T>) * sizeof(float);
+  return (kPair ? 8 : 4) * (size_t)kChunk<T> * D * sizeof(T) +
+         (sizeof(T) == 2 ? (kPair ? 2 : 1) * kBlocks<T> * (kFine ? 4096 : 2048) : 0) + (32 + 2 * kChunk<T>) * sizeof(float);
 }
 
 // kRev: from the last token to the first; kMany: y and z have the heads of the group (otherwise x has); kOut: rows are
 // written, otherwise the state alone is advanced.
+// kPair: two walks of one workgroup, half of its waves each, over the same two streams of tiles: y of the one is z of the other, the
+// other's state the transpose.  dk and dv read q and dout once that way (4 x 8k tokens, 16 heads: 375 us apart, 260 together).
 // Roundings in bf16 (sums and states are fp32 throughout): the state enters x S, and the decayed pairs of a chunk the product
 // with z, as one operand each, which leaves an output twice the variance of its own rounding; kFine: as two, with
 // errors of 2^-16, for prompts so short that an output rests on a few pairs.  The decayed z enters the state as three
 // operands, all 24 bits, where the state is a result, as two elsewhere (a.fine_state).
-template <typename T, int D, bool kRev, bool kMany, bool kOut, bool kFine>
-__global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
+template <typename T, int D, bool kRev, bool kMany, bool kOut, bool kPair, bool kFine>
+__global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(LinArgs a) {
   using Tl = Tile<T, D>;
   constexpr int NW = D / 32, C = kChunk<T>, TB = C / 32, KS = D / 16, NB = D / 32, SK = C / 16;
   constexpr uint32_t kTileB = C * Tl::kRowB;
@@ -71,13 +76,19 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   constexpr int kPlanes = Tl::kBf16 && kFine ? 2 : 1, kPlanesZ = Tl::kBf16 ? 3 : 1;
   constexpr bool kShare = Tl::kBf16;   // each pair block by one wave, passed on through LDS (fp32 has one block: every wave makes it)
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const uint32_t at_y = lds_addr_of(lds), at_z = at_y + 2 * kTileB, at_x = at_z + kTileB;
-  char *pairs = lds + 4 * kTileB;
-  float *rel = reinterpret_cast<float *>(pairs + (kShare ? kBlocks<T> * kPlanes * 2048 : 0));   // [32 + n]: scale e^{a n}, n = -32 .. C - 1
-  float *wt = rel + 32 + C;   // [i]: the decay of a chunk's token i in the state behind it
+  constexpr int kWaves = kPair ? 2 * NW : NW;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave_all = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool second = kPair && wave_all >= NW;          // of the pair's walks
+  const int wave = second ? wave_all - NW : wave_all;
+  // tiles: y twice, z, x (a pair, whose workgroup has its compute unit to itself: all of them twice)
+  const uint32_t at0 = lds_addr_of(lds), at_y = second ? at0 + 2 * kTileB : at0;
+  const uint32_t at_z = second ? at0 : at0 + 2 * kTileB, at_x = at0 + (kPair ? (second ? 6 : 4) : 3) * kTileB;
+  char *pairs = lds + (kPair ? 8 : 4) * kTileB + (second ? kBlocks<T> * kPlanes * 2048 : 0);
+  float *rel = reinterpret_cast<float *>(lds + (kPair ? 8 : 4) * kTileB + (kShare ? (kPair ? 2 : 1) * kBlocks<T> * kPlanes * 2048 : 0));   // [32 + n]: scale e^{a n}, n = -32 .. C - 1
+  float *wt = rel + 32 + C;   // [i]: the decay of a chunk's token i in the state behind it
   const int g = lane >> 5, l32 = lane & 31;
+  const bool transposed = kPair ? second : a.transposed != 0;
   // the lane's z channel of its wave's 32: such that results, which have z channels as rows, are in natural order
   const int zl = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
   const int u = blockIdx.x % a.units, seg = blockIdx.x / a.units;
@@ -94,19 +105,19 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   if constexpr (kOut) {   // rows behind the sequence
     const int z0 = s0 > n ? s0 : n, z1 = s0 + a.seg_tokens < a.T ? s0 + a.seg_tokens : a.T;
     constexpr int kParts = Tl::kRowB / 16;
-    for (int i = tid; i < (z1 - z0) * heads_x * kParts; i += 64 * NW) {
+    for (int i = 64 * wave + lane; i < (z1 - z0) * heads_x * kParts; i += 64 * NW) {
       const int part = i % kParts, hx = i / kParts % heads_x, t = z0 + i / (kParts * heads_x);
-      *reinterpret_cast<uint4 *>(a.out + b * a.o_b + (int64_t)t * a.o_t + (int64_t)(h * heads_x + hx) * a.o_h + 16 * part) =
+      *reinterpret_cast<uint4 *>((second ? a.out2 : a.out) + b * a.o_b + (int64_t)t * a.o_t + (int64_t)(h * heads_x + hx) * a.o_h + 16 * part) =
           make_uint4(0, 0, 0, 0);
     }
   }
-  const bool ends = kOut && a.end && (n > 0 ? s0 < n && n <= s0 + a.seg_tokens : seg == 0);
-  if (s0 >= n && !ends) return;
+  const bool ends = kOut && a.end && !second && (n > 0 ? s0 < n && n <= s0 + a.seg_tokens : seg == 0);
+  if (s0 >= n && !(kOut && a.end && n == 0 && seg == 0)) return;   // (an empty sequence's state is passed on)
   if (!kOut && s1 - s0 < a.seg_tokens) return;   // (a segment that another one follows is full)
 
   // ---- powers of the decay
   const float al = a.log_decay[h];
-  for (int i = tid; i < 32 + C; i += 64 * NW) rel[i] = i < 32 ? 0.f : a.scale * expf(al * (float)(i - 32));
+  for (int i = tid; i < 32 + C; i += 64 * kWaves) rel[i] = i < 32 ? 0.f : a.scale * expf(al * (float)(i - 32));
   if (tid < C) wt[tid] = expf(al * (float)(C - kShift - tid));
   float dec[TB];
 #pragma unroll
@@ -120,7 +131,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   // ---- the state: element v of block blk is (y channel 32 blk + 16 (v / 8) + 8 g + v % 8, z channel 32 wave + zl)
   f32x16 S[NB];
   {
-    const float *src = seg == 0 ? a.start : a.seg + ((int64_t)u * a.n_seg + seg) * (D * D);
+    const float *src = seg == 0 ? a.start : a.seg + ((int64_t)u * a.seg_of_unit + seg * a.seg_step) * (D * D);
     const float f = seg == 0 ? a.start_scale : 1.f;
     if (!kOut) src = nullptr;
     else if (seg == 0 && src) src += (int64_t)u * (D * D);
@@ -130,42 +141,43 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int yc = 32 * blk + 16 * (v >> 3) + 8 * g + (v & 7);
-        S[blk][v] = src ? f * src[a.transposed ? zc * D + yc : yc * D + zc] : 0.f;
+        S[blk][v] = src ? f * src[transposed ? zc * D + yc : yc * D + zc] : 0.f;
       }
   }
 
-  const char *xb = uniform_ptr(a.x + b * a.x_b + (int64_t)(h * heads_x) * a.x_h);
+  const char *xb = uniform_ptr((second ? a.x2 : a.x) + b * a.x_b + (int64_t)(h * heads_x) * a.x_h);
   const char *yb = uniform_ptr(a.y + b * a.y_b + (int64_t)(h * heads_y) * a.y_h);
   const char *zb = uniform_ptr(a.z + b * a.z_b + (int64_t)(h * heads_y) * a.z_h);
-  char *ob = a.out + b * a.o_b + (int64_t)(h * heads_x) * a.o_h;
+  char *ob = (second ? a.out2 : a.out) + b * a.o_b + (int64_t)(h * heads_x) * a.o_h;
   // first row in memory of the chunk at position c0 with nv tokens
   auto first_row = [&](int c0, int nv) { return kRev ? n - c0 - nv : c0; };
   auto load_yz = [&](int c0, int hd, uint32_t buf) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
     const int64_t r = first_row(c0, nv);
     const int ln = (int)here((uint32_t)lane);
-    Tl::template fill<C, NW, kRev>(yb + r * a.y_t + hd * a.y_h, (uint32_t)a.y_t, nv, at_y + buf * kTileB, wave, ln);
-    Tl::template fill<C, NW, kRev>(zb + r * a.z_t + hd * a.z_h, (uint32_t)a.z_t, nv, at_z, wave, ln);
+    Tl::template fill<C, kWaves, kRev>(yb + r * a.y_t + hd * a.y_h, (uint32_t)a.y_t, nv, at0 + buf * kTileB, wave_all, ln);
+    Tl::template fill<C, kWaves, kRev>(zb + r * a.z_t + hd * a.z_h, (uint32_t)a.z_t, nv, at0 + (2 + (kPair ? buf : 0)) * kTileB, wave_all, ln);
   };
-  auto load_x = [&](int c0, int hd) {
+  auto load_x = [&](int c0, int hd, [[maybe_unused]] uint32_t buf) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
-    Tl::template fill<C, NW, kRev>(xb + (int64_t)first_row(c0, nv) * a.x_t + hd * a.x_h, (uint32_t)a.x_t, nv, at_x, wave,
-                                   (int)here((uint32_t)lane));
+    Tl::template fill<C, NW, kRev>(xb + (int64_t)first_row(c0, nv) * a.x_t + hd * a.x_h, (uint32_t)a.x_t, nv, at_x + (kPair ? buf * kTileB : 0),
+                                   wave, (int)here((uint32_t)lane));
   };
 
-  Operand<T> xf[TB][KS], zf[SK];
+  Operand<T> xf[kPair ? 1 : TB][kPair ? 1 : KS], zf[SK];
   f32x16 o[TB];
-  uint32_t buf = 0;
+  uint32_t buf = 0, xbuf = 0;
   bool stored = false;   // full rows have been stored behind the latest loads
   const uint32_t lane_along = Tl::along0(lane), lane_across = Tl::template across0<false>(lane);
   // the decayed pairs of block (tb, sb) as operands of the second product: z^T . pairs
-  auto pairs_of = [&](auto tb_, auto sb_, uint32_t y_along, Operand<T> (&pw)[2][kPlanes]) {
+  auto pairs_of = [&](auto tb_, auto sb_, uint32_t y_along, [[maybe_unused]] uint32_t x_along, Operand<T> (&pw)[2][kPlanes]) {
     constexpr int tb = decltype(tb_)::value, sb = decltype(sb_)::value;
     f32x16 sc = {0.f};
-    // (many heads of y: x is in registers for the first of them alone, where the state is asked)
-    const uint32_t x = kMany && kShare ? here(at_x + lane_along) : 0;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sc = mma(Tl::along(y_along, sb, ks), kMany && kShare ? Tl::along(x, tb, ks) : xf[tb][ks], sc);
+    for (int ks = 0; ks < KS; ++ks) {
+      if constexpr (kPair) sc = mma(Tl::along(y_along, sb, ks), Tl::along(x_along, tb, ks), sc);
+      else sc = mma(Tl::along(y_along, sb, ks), xf[tb][ks], sc);
+    }
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       float w[8];
@@ -184,7 +196,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
   __syncthreads();
   if (s0 < s1) {
     load_yz(s0, 0, 0);
-    if constexpr (kOut) load_x(s0, 0);
+    if constexpr (kOut) load_x(s0, 0, 0);
   }
   for (int c0 = s0; c0 < s1; c0 += C) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
@@ -200,15 +212,54 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
       else wait_vmem<0>();
       publish();
       stored = false;
-      if (kOut && new_x) {
-        const uint32_t x = here(at_x + lane_along);
+      auto load_next = [&]() {
+        const int nc0 = last ? c0 + C : c0, nhd = last ? 0 : hd + 1;
+        if (nc0 < s1) {
+          if (kMany || nhd == 0) load_yz(nc0, nhd, buf ^ 1);
+          if (kOut && (!kMany || nhd == 0)) load_x(nc0, nhd, xbuf ^ 1);
+        }
+      };
+      if constexpr (kPair) load_next();
+      const uint32_t x_along = here(at_x + (kPair ? xbuf * kTileB : 0) + lane_along);
+      if constexpr (kOut && !kPair) {
+        if (new_x) {
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) xf[tb][ks] = Tl::along(x_along, tb, ks);
+        }
+      }
+      // o = x S, decayed
+      auto ask_state = [&]() {
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) o[tb] = f32x16{0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          float s[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[e] = S[ks >> 1][8 * (ks & 1) + e];
+          Operand<T> pl[kPlanes], x[TB];
+          split_operand<kPlanes>(s, pl);
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb) {
+            if constexpr (kPair) x[tb] = Tl::along(x_along, tb, ks);
+            else x[tb] = xf[tb][ks];
+          }
+#pragma unroll
+          for (int i = 0; i < kPlanes; ++i)
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) o[tb] = mma(pl[i], x[tb], o[tb]);
+        }
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) xf[tb][ks] = Tl::along(x, tb, ks);
+          for (int v = 0; v < 16; ++v) o[tb][v] *= dec[tb];
+      };
+      if constexpr (kPair) {
+        if (new_x) ask_state();
       }
       if (new_yz) {
-        const uint32_t z = here((at_z + lane_across) ^ (uint32_t)(32 * wave * (int)sizeof(T)));
+        const uint32_t z = here((at_z + (kPair ? buf * kTileB : 0) + lane_across) ^ (uint32_t)(32 * wave * (int)sizeof(T)));
 #pragma unroll
         for (int ks = 0; ks < SK; ++ks) zf[ks] = Tl::across(z, 0, ks);
       }
@@ -216,7 +267,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
       if constexpr (kOut && kShare) {
         auto pass_on = [&](int i, auto tb, auto sb) {
           Operand<T> pw[2][kPlanes];
-          pairs_of(tb, sb, y_along, pw);
+          pairs_of(tb, sb, y_along, x_along, pw);
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -227,34 +278,11 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
         if (wave == 0) pass_on(1, I1{}, I0{});
         if (wave == (NW > 2 ? 2 : 1)) pass_on(2, I1{}, I1{});
       }
-      publish();   // x and z of this step are in registers, its pairs in LDS
-      {
-        const int nc0 = last ? c0 + C : c0, nhd = last ? 0 : hd + 1;
-        if (nc0 < s1) {
-          if (kMany || nhd == 0) load_yz(nc0, nhd, buf ^ 1);
-          if (kOut && (!kMany || nhd == 0)) load_x(nc0, nhd);
-        }
-      }
+      publish();   // the step's pairs are in LDS, and where there is one tile of them, x and z in registers
+      if constexpr (!kPair) load_next();
       if constexpr (kOut) {
-        if (new_x) {   // x S
-#pragma unroll
-          for (int tb = 0; tb < TB; ++tb) o[tb] = f32x16{0.f};
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            float s[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] = S[ks >> 1][8 * (ks & 1) + e];
-            Operand<T> pl[kPlanes];
-            split_operand<kPlanes>(s, pl);
-#pragma unroll
-            for (int i = 0; i < kPlanes; ++i)
-#pragma unroll
-              for (int tb = 0; tb < TB; ++tb) o[tb] = mma(pl[i], xf[tb][ks], o[tb]);
-          }
-#pragma unroll
-          for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[tb][v] *= dec[tb];
+        if constexpr (!kPair) {
+          if (new_x) ask_state();
         }
         // the chunk's own tokens
         if constexpr (kShare) {
@@ -267,7 +295,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
                 o[i > 0] = mma(zf[(i == 2 ? 2 : 0) + hf], *reinterpret_cast<const Operand<T> *>(pairs + ((2 * i + hf) * kPlanes + pl) * 1024 + 16 * lane), o[i > 0]);
         } else {
           Operand<T> pw[2][kPlanes];
-          pairs_of(I0{}, I0{}, y_along, pw);
+          pairs_of(I0{}, I0{}, y_along, x_along, pw);
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) o[0] = mma(zf[hf], pw[hf][0], o[0]);
         }
@@ -334,6 +362,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
         }
       }
       if (kMany || last) buf ^= 1;
+      if (last) xbuf ^= 1;
     }
   }
   float *dst = nullptr;
@@ -344,7 +373,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_walk_kernel(LinArgs a) {
       f = a.end_scale;
     }
   } else {
-    dst = a.seg + ((int64_t)u * a.n_seg + seg) * (D * D);
+    dst = a.seg + ((int64_t)u * a.seg_of_unit + seg) * (D * D);
   }
   if (dst) {
 #pragma unroll
@@ -369,7 +398,7 @@ __global__ __launch_bounds__(256) void linear_segments_kernel(LinArgs a, int dd)
   }
   // segments that another one follows are full; eight of them are asked for at a time
   const int n_full = n > 0 ? (n - 1) / a.seg_tokens : -1;
-  float *at = a.seg + (int64_t)u * a.n_seg * dd + i;
+  float *at = a.seg + (int64_t)u * a.seg_of_unit * dd + i;
   constexpr int kAhead = 8;
   for (int seg0 = 0; seg0 <= n_full; seg0 += kAhead) {
     float4 add[kAhead];
@@ -491,30 +520,30 @@ size_t state_bytes(const kvm_linear_config *c) {
   return (size_t)c->batch * c->n_kv_heads * c->head_dim * c->head_dim * sizeof(float);
 }
 
-template <typename T, int D, bool kRev, bool kMany, bool kOut, bool kFine>
+template <typename T, int D, bool kRev, bool kMany, bool kOut, bool kPair, bool kFine>
 hipError_t launch_walk_as(const LinArgs &a, int n_wg, hipStream_t st) {
   static OncePerDevice<hipError_t> once;
-  constexpr size_t bytes = linear_lds<T, D, kFine>();
-  hipError_t e = allow_lds(once, (const void *)linear_walk_kernel<T, D, kRev, kMany, kOut, kFine>, bytes);
+  constexpr size_t bytes = linear_lds<T, D, kPair, kFine>();
+  hipError_t e = allow_lds(once, (const void *)linear_walk_kernel<T, D, kRev, kMany, kOut, kPair, kFine>, bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((linear_walk_kernel<T, D, kRev, kMany, kOut, kFine>), dim3((unsigned)n_wg), dim3(2 * D), bytes, st, a);
+  hipLaunchKernelGGL((linear_walk_kernel<T, D, kRev, kMany, kOut, kPair, kFine>), dim3((unsigned)n_wg), dim3(kPair ? 4 * D : 2 * D), bytes, st, a);
   return hipGetLastError();
 }
 // Prompts of up to kFineTokens tokens are a few chunks long and wait for latencies: two more operands for each product cost
 // them nothing that shows.  Longer ones have many pairs behind most outputs, and the roundings of these average out.
 constexpr int kFineTokens = 128;
-template <bool kRev, bool kMany, bool kOut>
+template <bool kRev, bool kMany, bool kOut, bool kPair>
 hipError_t launch_walk(const kvm_linear_config *c, const LinArgs &a, int n_wg, hipStream_t st) {
   if (c->io_dtype == KVM_F32)
-    return c->head_dim == 128 ? launch_walk_as<float, 128, kRev, kMany, kOut, false>(a, n_wg, st)
-                              : launch_walk_as<float, 64, kRev, kMany, kOut, false>(a, n_wg, st);
+    return c->head_dim == 128 ? launch_walk_as<float, 128, kRev, kMany, kOut, kPair, false>(a, n_wg, st)
+                              : launch_walk_as<float, 64, kRev, kMany, kOut, kPair, false>(a, n_wg, st);
   if constexpr (kOut) {
     if (a.T <= kFineTokens)
-      return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut, true>(a, n_wg, st)
-                                : launch_walk_as<bf16_t, 64, kRev, kMany, kOut, true>(a, n_wg, st);
+      return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut, kPair, true>(a, n_wg, st)
+                                : launch_walk_as<bf16_t, 64, kRev, kMany, kOut, kPair, true>(a, n_wg, st);
   }
-  return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut, false>(a, n_wg, st)
-                            : launch_walk_as<bf16_t, 64, kRev, kMany, kOut, false>(a, n_wg, st);
+  return c->head_dim == 128 ? launch_walk_as<bf16_t, 128, kRev, kMany, kOut, kPair, false>(a, n_wg, st)
+                            : launch_walk_as<bf16_t, 64, kRev, kMany, kOut, kPair, false>(a, n_wg, st);
 }
 hipError_t launch_segments(const kvm_linear_config *c, const LinArgs &a, hipStream_t st) {
   const int dd = c->head_dim * c->head_dim;
@@ -577,14 +606,14 @@ extern "C" int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, c
   a.log_decay = log_decay; a.lens = lens; a.start = state_in; a.seg = (float *)workspace; a.end = state_out; a.fine_state = state_out != nullptr;
   a.start_scale = a.end_scale = 1.f; a.scale = scale_of(cfg);
   a.T = (int32_t)T; a.H = (int32_t)hk; a.G = (int32_t)(hq / hk); a.units = cfg->batch * cfg->n_kv_heads;
-  a.n_seg = cut.n_seg; a.seg_tokens = cut.seg_tokens;
+  a.n_seg = a.seg_of_unit = cut.n_seg; a.seg_tokens = cut.seg_tokens; a.seg_step = 1;
   hipStream_t st = (hipStream_t)stream;
   hipError_t e = hipSuccess;
   if (cut.n_seg > 1) {
-    e = launch_walk<false, false, false>(cfg, a, a.units * (a.n_seg - 1), st);
+    e = launch_walk<false, false, false, false>(cfg, a, a.units * (a.n_seg - 1), st);
     if (e == hipSuccess) e = launch_segments(cfg, a, st);
   }
-  if (e == hipSuccess) e = launch_walk<false, false, true>(cfg, a, a.units * a.n_seg, st);
+  if (e == hipSuccess) e = launch_walk<false, false, true, false>(cfg, a, a.units * a.n_seg, st);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_linear_prefill");
 }
 
@@ -608,7 +637,7 @@ extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, 
   LinArgs c = {};
   c.log_decay = log_decay; c.lens = lens; c.seg = (float *)workspace; c.scale = scale;
   c.T = (int32_t)T; c.H = (int32_t)hk; c.G = (int32_t)(hq / hk); c.units = cfg->batch * cfg->n_kv_heads;
-  c.n_seg = cut.n_seg; c.seg_tokens = cut.seg_tokens;
+  c.n_seg = c.seg_of_unit = cut.n_seg; c.seg_tokens = cut.seg_tokens; c.seg_step = 1;
   auto roles = [&](const void *x, bool xq, const void *y, bool yq, const void *z, bool zq, void *o) {
     LinArgs a = c;
     auto put = [&](bool is_q, int64_t &sb, int64_t &s_t, int64_t &sh) {
@@ -626,24 +655,24 @@ extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, 
   LinArgs f = roles(q, true, k, false, v, false, dq);
   f.start = state_in; f.start_scale = f.end_scale = 1.f;
   if (cut.n_seg > 1 && !kept) {
-    e = launch_walk<false, false, false>(cfg, f, f.units * (f.n_seg - 1), st);
+    e = launch_walk<false, false, false, false>(cfg, f, f.units * (f.n_seg - 1), st);
     if (e == hipSuccess) e = launch_segments(cfg, f, st);
   }
   LinArgs a = roles(dout, true, v, false, k, false, dq);
   a.start = state_in; a.start_scale = 1.f; a.transposed = 1;
   if (kept) a.seg = (float *)const_cast<void *>(kept);   // (read alone)
-  if (e == hipSuccess) e = launch_walk<false, false, true>(cfg, a, a.units * a.n_seg, st);
+  if (e == hipSuccess) e = launch_walk<false, false, true, false>(cfg, a, a.units * a.n_seg, st);
   // dv and dk: backwards; the state there is that of the products q dout, without the scale
   LinArgs r = roles(k, false, q, true, dout, true, dv);
+  r.x2 = (const char *)v; r.out2 = (char *)dk;
   r.start = dstate_out; r.start_scale = 1.f / scale; r.end = dstate_in; r.end_scale = scale; r.fine_state = dstate_in != nullptr;
   if (cut.n_seg > 1) {
-    if (e == hipSuccess) e = launch_walk<true, true, false>(cfg, r, r.units * (r.n_seg - 1), st);
+    if (e == hipSuccess) e = launch_walk<true, true, false, false>(cfg, r, r.units * (r.n_seg - 1), st);
     if (e == hipSuccess) e = launch_segments(cfg, r, st);
   }
-  if (e == hipSuccess) e = launch_walk<true, true, true>(cfg, r, r.units * r.n_seg, st);
-  LinArgs t = roles(v, false, dout, true, q, true, dk);
-  t.start = dstate_out; t.start_scale = 1.f / scale; t.transposed = 1;
-  if (e == hipSuccess) e = launch_walk<true, true, true>(cfg, t, t.units * t.n_seg, st);
+  // (a pair of walks has twice the waves of one: half as many segments fill the device)
+  r.n_seg = (r.n_seg + 1) / 2; r.seg_tokens *= 2; r.seg_step = 2;
+  if (e == hipSuccess) e = launch_walk<true, true, true, true>(cfg, r, r.units * r.n_seg, st);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_linear_backward");
 }
 

@@ -40,6 +40,8 @@ struct WinArgs {
   float *part;     // [units, parts, 2, sink_rows, D]: shares of the sinks' dk and dv, the last from the queries of their window
   int32_t n_split, split_q;   // ranges that the queries beyond a sink's window are cut into, and their length
   int32_t sink_rows, parts;   // S up to 32, 64 or 128; shares
+  float *sums;     // n_part > 1: [units, n_part, 2, Tk, D]: dk and dv of every part of a key tile's queries
+  int32_t n_part;
   int32_t key_tiles;
 };
 
@@ -524,8 +526,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
   const int g = lane >> 5, l32 = lane & 31;
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq, units = a.B * a.Hkv;
   // a unit's workgroups go to one XCD
-  const int per_unit = far ? a.n_split : a.key_tiles;
-  const int u = blockIdx.x / kXcds / per_unit * kXcds + blockIdx.x % kXcds, member = blockIdx.x / kXcds % per_unit;
+  const int per_unit = far ? a.n_split : a.key_tiles * a.n_part;
+  const int u = blockIdx.x / kXcds / per_unit * kXcds + blockIdx.x % kXcds;
+  const int member = blockIdx.x / kXcds % per_unit / (far ? 1 : a.n_part), queries = blockIdx.x / kXcds % (far ? 1 : a.n_part);
   if (u >= units) return;
   const int b = u / a.Hkv, hkv = u % a.Hkv;
   const int n = tokens_of(a, b);
@@ -545,7 +548,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
   t0 = t0 > off ? t0 : off;
   t1 = t1 < n ? t1 : n;
   const int n_rows = kend > K0 && t1 > t0 ? t1 - t0 : 0;
-  const int n_tiles = (n_rows + 31) / 32 * G;
+  // this workgroup's tiles, of 32 queries of a head: those from it0 on of all
+  const int all_tiles = (n_rows + 31) / 32 * G, per_part = far ? all_tiles : (all_tiles + a.n_part - 1) / a.n_part;
+  const int it0 = far ? 0 : queries * per_part;
+  const int n_tiles = all_tiles - it0 < per_part ? all_tiles - it0 : per_part;
 
   f32x16 dk[DB], dv[DB];
 #pragma unroll
@@ -558,7 +564,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
     const char *qb = uniform_ptr(a.q + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
     const char *db = uniform_ptr(a.dout + b * a.o_b + (int64_t)(hkv * G) * a.o_h + (int64_t)(t0 - off) * a.o_t);
     // the tile asked for last: 32 queries from t0 + str_row on, of one head
-    int str_row = 0, str_head = 0;
+    int str_row = it0 / G * 32, str_head = it0 % G;
     // lse (the lower half of the wave) or D of its rows
     auto row_value = [&]() {
       int r = str_row + l32;
@@ -692,6 +698,19 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
 #pragma unroll
       for (int v = 0; v < 16; ++v) dk[i][v] *= a.scale;
   }
+  if (!far && a.n_part > 1) {   // added up by window_sum_kernel
+    if (key < a.Tk) {
+      float *pk = a.sums + (((int64_t)u * a.n_part + queries) * 2 * a.Tk + key) * D;
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+        const f32x16 &x = dk[i >> 2], &y = dv[i >> 2];
+        const int v = 4 * (i & 3);
+        store4<float>((char *)pk, i >> 2, i & 3, g, x[v], x[v + 1], x[v + 2], x[v + 3]);
+        store4<float>((char *)(pk + (int64_t)a.Tk * D), i >> 2, i & 3, g, y[v], y[v + 1], y[v + 2], y[v + 3]);
+      }
+    }
+    return;
+  }
   if (far || key < a.S) {   // a sink's share
     if (key < a.S) {
       const int share = far ? member * (kWaves / n_kb) + tw : a.parts - 1;
@@ -725,6 +744,30 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
       }
     }
   }
+}
+
+// dk and dv where a key tile's queries are shared among workgroups: the sums of the parts, and of a sink's far shares.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_sum_kernel(WinArgs a) {
+  const int u = blockIdx.y, b = u / a.Hkv, hkv = u % a.Hkv;
+  const int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x), n = (int64_t)a.Tk * D;
+  if (i >= 2 * n) return;
+  const int which = i >= n, key = (int)((i - which * n) / D), ch = (int)(i % D);
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](const float *p) {
+    const float4 y = *reinterpret_cast<const float4 *>(p);
+    x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w;
+  };
+  if (key < tokens_of(a, b)) {
+#pragma unroll 4
+    for (int s = 0; s < a.n_part; ++s) add(a.sums + ((int64_t)u * a.n_part + s) * 2 * n + i);
+    if (key < a.S)
+#pragma unroll 4
+      for (int s = 0; s + 1 < a.parts; ++s) add(a.part + ((((int64_t)u * a.parts + s) * 2 + which) * a.sink_rows + key) * D + ch);
+  }
+  char *row = which ? a.dv + b * a.v_b + (int64_t)key * a.v_t + (int64_t)hkv * a.v_h
+                    : a.dk + b * a.k_b + (int64_t)key * a.k_t + (int64_t)hkv * a.k_h;
+  store4<T>(row + ch * (int)sizeof(T), 0, 0, 0, x[0], x[1], x[2], x[3]);
 }
 
 // dk and dv of the sinks: the sums of their shares, four of them for every value, and these added.
@@ -1019,11 +1062,19 @@ unsigned query_grid(const WinArgs &a) {
 // workgroups to a compute unit) and 64 at most.
 void cut_far(WinArgs &a) {
   a.key_tiles = (a.Tk + 127) / 128;
+  // Few key tiles: the queries of each are shared among as many workgroups as give the device two to a compute unit, four tiles at
+  // least to each.  (3 sequences of 777 tokens, 2 KV heads, fp32: 150 us
+  // with 42 workgroups, 44 in 8 parts and 6 for their sum.)
+  const int64_t units = (int64_t)a.B * a.Hkv, wgs = units * a.key_tiles;
+  const int64_t stream = (int64_t)((a.W + 127 < a.Tk ? a.W + 127 : a.Tk) + 31) / 32 * (a.Hq / a.Hkv);
+  a.n_part = 1;
+  if (wgs < 256) a.n_part = (int32_t)(512 / wgs < stream / 4 ? 512 / wgs : stream / 4);
+  if (a.n_part < 1) a.n_part = 1;
   a.sink_rows = 32;
   if (a.S == 0) return;
   a.sink_rows = a.S <= 32 ? 32 : a.S <= 64 ? 64 : 128;
   const int step = kWaves / (a.sink_rows / 32), far = a.Tk - a.W;
-  const int64_t units = (int64_t)a.B * a.Hkv, most = units < 8 ? 64 : units < 512 ? 512 / units : 1;
+  const int64_t most = units < 8 ? 64 : units < 512 ? 512 / units : 1;
   a.split_q = (int32_t)((far + most - 1) / most + 32 * step - 1) / (32 * step) * (32 * step);
   a.n_split = (far + a.split_q - 1) / a.split_q;
   a.parts = a.n_split * step + 1;
@@ -1031,6 +1082,9 @@ void cut_far(WinArgs &a) {
 size_t delta_bytes(const WinArgs &a) { return ((size_t)a.B * a.Hq * a.Tq * sizeof(float) + 255) & ~(size_t)255; }
 size_t part_bytes(const WinArgs &a, int d) {
   return (size_t)a.B * a.Hkv * a.parts * 2 * a.sink_rows * d * sizeof(float);
+}
+size_t sums_bytes(const WinArgs &a, int d) {
+  return a.n_part > 1 ? (size_t)a.B * a.Hkv * a.n_part * 2 * a.Tk * d * sizeof(float) : 0;
 }
 
 template <typename T, int D>
@@ -1053,12 +1107,19 @@ hipError_t run_backward_as(const WinArgs &a, unsigned grid, unsigned units8, hip
   hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D, false>), dim3(units8 * a.key_tiles), dim3(256), bytes_kv, st, a);
+  hipLaunchKernelGGL((window_dkv_kernel<T, D, false>), dim3(units8 * a.key_tiles * a.n_part), dim3(256), bytes_kv, st, a);
   e = hipGetLastError();
-  if (e != hipSuccess || a.n_split == 0) return e;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D, true>), dim3(units8 * a.n_split), dim3(256), bytes_kv, st, a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || (a.n_split == 0 && a.n_part == 1)) return e;
+  if (a.n_split > 0) {
+    hipLaunchKernelGGL((window_dkv_kernel<T, D, true>), dim3(units8 * a.n_split), dim3(256), bytes_kv, st, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.n_part > 1) {
+    const unsigned wgs = (unsigned)((2 * (int64_t)a.Tk * D / 4 + 255) / 256);
+    hipLaunchKernelGGL((window_sum_kernel<T, D>), dim3(wgs, (unsigned)(a.B * a.Hkv)), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL((window_sinks_kernel<T, D>), dim3((unsigned)(2 * a.S * D / 64), (unsigned)(a.B * a.Hkv)), dim3(256), 0,
                      st, a);
   return hipGetLastError();
@@ -1130,7 +1191,7 @@ extern "C" size_t kvm_window_backward_workspace_bytes(const kvm_window_config *c
   if (!valid(cfg) || !lengths_ok(Tq, Tk)) return 0;
   WinArgs a = base_args(cfg, Tq, Tk, nullptr);
   cut_far(a);
-  return delta_bytes(a) + part_bytes(a, cfg->head_dim);
+  return delta_bytes(a) + part_bytes(a, cfg->head_dim) + sums_bytes(a, cfg->head_dim);
 }
 
 extern "C" int kvm_window_backward(const kvm_window_config *cfg, const void *q, const void *k, const void *v, const int32_t *lens,
@@ -1157,6 +1218,7 @@ extern "C" int kvm_window_backward(const kvm_window_config *cfg, const void *q, 
   a.l_b = Tq * hq; a.l_t = hq; a.l_h = 1;
   a.delta = (float *)workspace;
   a.part = (float *)((char *)workspace + delta_bytes(a));
+  a.sums = (float *)((char *)a.part + part_bytes(a, (int)d));
   const unsigned grid = query_grid(a);
   const int64_t units8 = ((int64_t)a.B * a.Hkv + kXcds - 1) / kXcds * kXcds;
   if (grid == 0 || units8 * a.key_tiles >= (1ll << 31) || (int64_t)a.B * a.Hkv > 65535) return KVM_ERR_ARG;

@@ -61,6 +61,12 @@ def kvm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gate: Optio
     return _KVMAttention.apply(q, k, v, gate, ln_gamma, ln_beta, tau_state, tau_bswa, cfg)
 
 
+def _once(ctx) -> None:
+    """A gradient of these gradients does not exist: refused where one is asked for (create_graph), not left out."""
+    if torch.is_grad_enabled():
+        raise RuntimeError(f"{type(ctx).__name__}: the gradients are not differentiable again (create_graph)")
+
+
 class _LinearAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, log_decay, state, lens, scale):
@@ -73,8 +79,8 @@ class _LinearAttention(torch.autograd.Function):
         return out, end
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dout, dend):
+        _once(ctx)
         q, k, v, log_decay, state, lens, kept = ctx.saved_tensors
         dout = torch.zeros_like(q) if dout is None else dout.contiguous()
         dend = None if dend is None else dend.contiguous()
@@ -105,8 +111,8 @@ class _WindowAttention(torch.autograd.Function):
         return out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
+        _once(ctx)
         q, k, v, lens, out, rest, lse = ctx.saved_tensors
         dq, dk, dv = window_backward(q, k, v, out, lse, dout.contiguous(), window=ctx.window, n_sink=ctx.n_sink, lens=lens,
                                      scale=ctx.scale, out_rest=rest)

@@ -653,8 +653,8 @@ def _heads(q: torch.Tensor, k: torch.Tensor, dims: int):
 
 
 def _row_strides(q, k, v, out, lse=None) -> kvm_strides:
-    bth = lambda t: (0, 0, 0) if t is None else (t.stride(0), t.stride(1), t.stride(2))
-    return kvm_strides(*bth(q), *bth(k), *bth(v), *bth(out), 0, 0, 0, *bth(lse))
+    return kvm_strides(*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *out.stride()[:3], 0, 0, 0,
+                       *((0, 0, 0) if lse is None else lse.stride()))
 
 
 @functools.lru_cache(maxsize=4096)

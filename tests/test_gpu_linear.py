@@ -280,3 +280,15 @@ def test_refusals_by_the_binding():
     with pytest.raises(kvm.KVMError):   # rows that start off a 16-byte border
         wide = torch.zeros(2, 8, 4, 70, dtype=torch.bfloat16, device=DEV)
         kvm.linear_prefill(wide[..., 1:65], x["k"], x["v"], x["log_decay"])
+
+
+def test_gradients_of_gradients_are_refused_and_a_graph_can_be_used_twice():
+    import paper_2605_09877_amd as kvm
+    x = make("f32", 1, 40, 2, 1, 64)
+    leaves = [x[n].clone().requires_grad_() for n in "qkv"]
+    out = kvm.kvm_linear_attention(*leaves, x["log_decay"])[0]
+    first = torch.autograd.grad(out, leaves, x["dout"], retain_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(out, leaves, x["dout"], retain_graph=True, create_graph=True)
+    for a, b in zip(first, torch.autograd.grad(out, leaves, x["dout"])):
+        assert torch.equal(a, b)

@@ -353,3 +353,15 @@ def test_refusals_by_the_binding():
         kvm.window_decode(ck, cv, *[x[n][:, 0].contiguous() for n in "qkv"], torch.zeros(2, device=DEV), window=4)
     with pytest.raises(ValueError):
         kvm.window_fill(ck, cv, x["k"], x["v"], window=5)
+
+
+def test_gradients_of_gradients_are_refused_and_a_graph_can_be_used_twice():
+    import paper_2605_09877_amd as kvm
+    x = make("f32", 1, 40, 40, 2, 1, 64)
+    leaves = [x[n].clone().requires_grad_() for n in "qkv"]
+    out = kvm.kvm_window_attention(*leaves, window=9)
+    first = torch.autograd.grad(out, leaves, x["dout"], retain_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(out, leaves, x["dout"], retain_graph=True, create_graph=True)
+    for a, b in zip(first, torch.autograd.grad(out, leaves, x["dout"])):
+        assert torch.equal(a, b)

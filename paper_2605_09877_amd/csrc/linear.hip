@@ -396,10 +396,10 @@ __global__ __launch_bounds__(256) void linear_segments_kernel(LinArgs a, int dd)
     s = *reinterpret_cast<const float4 *>(a.start + (int64_t)u * dd + i);
     s.x *= a.start_scale; s.y *= a.start_scale; s.z *= a.start_scale; s.w *= a.start_scale;
   }
-  // segments that another one follows are full; eight of them are asked for at a time
+  // segments that another one follows are full; sixteen of them are asked for at a time
   const int n_full = n > 0 ? (n - 1) / a.seg_tokens : -1;
   float *at = a.seg + (int64_t)u * a.seg_of_unit * dd + i;
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 16;
   for (int seg0 = 0; seg0 <= n_full; seg0 += kAhead) {
     float4 add[kAhead];
 #pragma unroll

@@ -370,12 +370,206 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 2) void window_pref
   write_query<T, D>(a, orow, lse, o, m, l, g);
 }
 
+// The same where there are few queries: the four waves of a workgroup take the same 32 queries of one head and a quarter of the key tiles
+// each, in LDS of their own and without a barrier, and their results are joined in the end.  What bounds such calls is the time of one
+// workgroup's loop, which is a quarter as long.
+template <typename T, int D>
+constexpr size_t split_lds() {
+  return kWaves * (2 * (size_t)kPromptRows<T, D> * D * sizeof(T) + 2 * 64 * sizeof(float)) + 32 * sizeof(int);
+}
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_prefill_split_kernel(WinArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int KT = kPromptRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr uint32_t kTileB = KT * Tl::kRowB;
+  constexpr int kLoads = (int)(kTileB / 1024);   // of a wave for a tile
+  static_assert(2 * kTileB >= 64 * 16 * DB * sizeof(float), "a wave's result fits its tiles");
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const uint32_t at_k = lds_addr_of(lds) + (uint32_t)wave * (2 * kTileB), at_v = at_k + kTileB;
+  float *stats = reinterpret_cast<float *>(lds + kWaves * 2 * kTileB);   // [wave][m | l][lane]
+  int *redo = reinterpret_cast<int *>(stats + kWaves * 128);             // [query]
+  const Item w(a);
+  if (w.none) return;
+  const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
+  const int n = tokens_of(a, w.b);
+  const int nq = n - off < 0 ? 0 : n - off;
+  const int Q0 = w.tile * 32, Q1 = Q0 + 32 < nq ? Q0 + 32 : nq;
+  const int hq = w.hkv * G + w.head, myq = Q0 + l32, t = myq + off;
+  char *orow = a.out + w.b * a.o_b + (int64_t)myq * a.o_t + (int64_t)hq * a.o_h;
+  float *lse = a.lse ? a.lse + w.b * a.l_b + (int64_t)myq * a.l_t + (int64_t)hq * a.l_h : nullptr;
+  if (wave == 0 && myq >= nq && myq < a.Tq) {   // behind the sequence
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) store4<T>(orow, i >> 2, i & 3, g, 0.f, 0.f, 0.f, 0.f);
+    if (lse && g == 0) *lse = -INFINITY;
+  }
+  if (Q0 >= nq) return;
+  if (tid < 32) redo[tid] = 0;
+  const KeyTiles keys(a, Q0 + off, Q1 + off, KT);
+  const int n_tiles = __builtin_amdgcn_readfirstlane(keys.n_tiles);
+  const char *kb = uniform_ptr(a.k + w.b * a.k_b + (int64_t)w.hkv * a.k_h);
+  const char *vb = uniform_ptr(a.v + w.b * a.v_b + (int64_t)w.hkv * a.v_h);
+  auto load_k = [&](int it) {
+    const int j0 = keys.first(it, KT);
+    Tl::template fill<KT, 1, false>(kb + (int64_t)j0 * a.k_t, (uint32_t)a.k_t, keys.end(it) - j0, at_k, 0, lane);
+  };
+  auto load_v = [&](int it) {
+    const int j0 = keys.first(it, KT);
+    Tl::template fill<KT, 1, false>(vb + (int64_t)j0 * a.v_t, (uint32_t)a.v_t, keys.end(it) - j0, at_v, 0, lane);
+  };
+  Operand<T> qf[KS];
+  const char *qrow = a.q + w.b * a.q_b + (int64_t)(myq < nq ? myq : nq - 1) * a.q_t + (int64_t)hq * a.q_h;
+  load_row<T, D>(qrow, g, qf);
+  const float c = a.scale * kLog2e;
+  f32x16 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) o[i] = f32x16{0.f};
+  float m = -INFINITY, l = 0.f;
+  const Fragments<T, D> fr(at_k, at_v, lane);
+  __builtin_amdgcn_s_waitcnt(0);
+  if (wave < n_tiles) {
+    load_k(wave);
+    load_v(wave);
+  }
+  for (int it = wave; it < n_tiles; it += kWaves) {
+    const bool more = it + kWaves < n_tiles;
+    const int j0 = keys.first(it, KT), j1 = keys.end(it);
+    wait_vmem<kLoads>();   // k (v was asked for behind it)
+    f32x16 s[NB];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) s[blk] = mma(fr.along(blk, ks, 0), qf[ks], ks == 0 ? f32x16{0.f} : s[blk]);
+    if (!(j0 + KT <= j1 && j0 + KT - 1 <= off + Q0 && (off + Q0 + 31 - j0 < a.W || j0 + KT <= a.S))) {
+      const int last = (t < j1 - 1 ? t : j1 - 1) - j0 - 4 * g, first = t - a.W + 1 - j0 - 4 * g, sink = a.S - j0 - 4 * g;
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = 32 * blk + mfma_row(v, 0);
+          s[blk][v] = r <= last && (r >= first || r < sink) ? s[blk][v] : -INFINITY;
+        }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the k tile has been read
+    if (more) load_k(it + kWaves);
+    float top = s[0][0];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, s[blk][v]);
+    const float m_new = fmaxf(m, xhalf_max(top) * c);
+    const float ref = m_new == -INFINITY ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m - ref);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[i][v] *= alpha;
+    if (more) wait_vmem<kLoads>();   // v (the next k was asked for behind it)
+    else wait_vmem<0>();
+#pragma unroll
+    for (int ks = 0; ks < 2 * NB; ++ks) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + e], c, -ref));
+      Operand<T> pf;
+      to_operand(p, pf);
+      if constexpr (sizeof(T) == 2) {
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pf.f.w[e]), ones, l, false);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) l += p[e];
+      }
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] = mma(fr.across(i, ks, 0), pf, o[i]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the v tile has been read
+    if (more) load_v(it + kWaves);
+  }
+  // every wave's result, then a block of channels by each of them
+  float *mine = reinterpret_cast<float *>(lds + wave * 2 * kTileB);
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mine[(16 * i + v) * 64 + lane] = o[i][v];
+  stats[wave * 128 + lane] = m;
+  stats[wave * 128 + 64 + lane] = xhalf_sum(l);
+  __syncthreads();
+  m = -INFINITY;
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) m = fmaxf(m, stats[x * 128 + lane]);
+  l = 0.f;
+  float f[kWaves];
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) {
+    f[x] = stats[x * 128 + lane] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[x * 128 + lane] - m);
+    l = fmaf(f[x], stats[x * 128 + 64 + lane], l);
+  }
+  f32x16 sum = {0.f};
+  if (wave < DB) {
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) {
+      const float *theirs = reinterpret_cast<const float *>(lds + x * 2 * kTileB) + 16 * wave * 64 + lane;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum[v] = fmaf(f[x], theirs[v * 64], sum[v]);
+    }
+    float bad = 0.f * l;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) bad = fmaf(sum[v], 0.f, bad);
+    if (!(xhalf_sum(bad) == 0.f)) redo[l32] = 1;
+  }
+  __syncthreads();
+  if (myq >= nq) return;
+  if (redo[l32]) {
+    if (wave == 0) {
+      attend_one_by_one<T, D>(a, qrow, kb, vb, t, c, g, o, m, l);
+      write_query<T, D>(a, orow, lse, o, m, l, g);
+    }
+    return;
+  }
+  if (wave < DB) {
+    o[0] = sum;
+    write_query<T, 32>(a, orow + 32 * wave * (int)sizeof(T), wave == 0 ? lse : nullptr, reinterpret_cast<const f32x16(&)[1]>(o[0]), m, l, g);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------
 // Gradients.  P = 2^(S scale log2 e - lse log2 e) is formed again; D = dout . out of a query, out with what its rounding left;
 //   dS = P (dP - D),  dq = scale dS K (queries stay, keys stream),  dk = scale dS^T q, dv = P^T dout (keys stay, queries stream).
 // P and dS enter their products in the I/O dtype.
 // (a query all of whose logits are -infinity has nothing of any key: P = 0)
 __device__ __forceinline__ float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// The lane's query for the dq kernels: q and dout, lse in powers of two, D = dout . out.
+template <typename T, int D>
+__device__ __forceinline__ void load_query(const WinArgs &a, int b, int hq, int myq, int nq, int g, Operand<T> (&qf)[D / 16],
+                                           Operand<T> (&df)[D / 16], float &lse2, float &delta) {
+  const int qc = myq < nq ? myq : nq - 1;
+  const int64_t at = b * a.o_b + (int64_t)qc * a.o_t + (int64_t)hq * a.o_h;
+  load_row<T, D>(a.q + at, g, qf);
+  load_row<T, D>(a.dout + at, g, df);
+  lse2 = lse_log2(a.lse[b * a.l_b + (int64_t)qc * a.l_t + (int64_t)hq * a.l_h]);
+  delta = 0.f;
+  auto add = [&](const char *row) {
+    Operand<T> of[D / 16];
+    load_row<T, D>(row, g, of);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      float x[8], y[8];
+      from_operand(of[ks], x);
+      from_operand(df[ks], y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(x[e], y[e], delta);
+    }
+  };
+  add(a.out + at);
+  if (sizeof(T) == 2 && a.rest) add(a.rest + at);
+  delta = xhalf_sum(delta);
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_kernel(WinArgs a) {
@@ -413,39 +607,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
   };
   load_tile(0);
   Operand<T> qf[KS], df[KS];
-  float lse2, delta = 0.f;
-  {
-    const int qc = myq < nq ? myq : nq - 1;
-    const int64_t at = w.b * a.o_b + (int64_t)qc * a.o_t + (int64_t)hq * a.o_h;
-    load_row<T, D>(a.q + at, g, qf);
-    load_row<T, D>(a.dout + at, g, df);
-    lse2 = lse_log2(a.lse[w.b * a.l_b + (int64_t)qc * a.l_t + (int64_t)hq * a.l_h]);
-    Operand<T> of[KS];
-    load_row<T, D>(a.out + at, g, of);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      float x[8], y[8];
-      from_operand(of[ks], x);
-      from_operand(df[ks], y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) delta = fmaf(x[e], y[e], delta);
-    }
-    if constexpr (sizeof(T) == 2) {
-      if (a.rest) {
-        load_row<T, D>(a.rest + at, g, of);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          float x[8], y[8];
-          from_operand(of[ks], x);
-          from_operand(df[ks], y);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) delta = fmaf(x[e], y[e], delta);
-        }
-      }
-    }
-    delta = xhalf_sum(delta);
-    if (myq < nq && g == 0) a.delta[((int64_t)w.b * a.Hq + hq) * a.Tq + myq] = delta;
-  }
+  float lse2, delta;
+  load_query<T, D>(a, w.b, hq, myq, nq, g, qf, df, lse2, delta);
+  if (myq < nq && g == 0) a.delta[((int64_t)w.b * a.Hq + hq) * a.Tq + myq] = delta;
   const float c = a.scale * kLog2e;
   f32x16 o[DB];
 #pragma unroll
@@ -503,6 +667,106 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
   for (int i = 0; i < 4 * DB; ++i)
     store4<T>(a.dq + at_row, i >> 2, i & 3, g, a.scale * o[i >> 2][4 * (i & 3)], a.scale * o[i >> 2][4 * (i & 3) + 1],
               a.scale * o[i >> 2][4 * (i & 3) + 2], a.scale * o[i >> 2][4 * (i & 3) + 3]);
+}
+
+// dq where there are few queries: waves share the key tiles of 32 queries, as in window_prefill_split_kernel.
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_split_kernel(WinArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int KT = kPromptRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr uint32_t kTileB = KT * Tl::kRowB;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, l32 = lane & 31;
+  const uint32_t at_k = lds_addr_of(lds) + (uint32_t)wave * (2 * kTileB), at_v = at_k + kTileB;
+  const Item w(a);
+  if (w.none) return;
+  const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq;
+  const int n = tokens_of(a, w.b);
+  const int nq = n - off < 0 ? 0 : n - off;
+  const int Q0 = w.tile * 32, Q1 = Q0 + 32 < nq ? Q0 + 32 : nq;
+  const int hq = w.hkv * G + w.head, myq = Q0 + l32, t = myq + off;
+  char *row = a.dq + w.b * a.o_b + (int64_t)myq * a.o_t + (int64_t)hq * a.o_h;
+  if (wave == 0 && myq >= nq && myq < a.Tq) {
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) store4<T>(row, i >> 2, i & 3, g, 0.f, 0.f, 0.f, 0.f);
+  }
+  if (Q0 >= nq) return;
+  const KeyTiles keys(a, Q0 + off, Q1 + off, KT);
+  const int n_tiles = __builtin_amdgcn_readfirstlane(keys.n_tiles);
+  const char *kb = uniform_ptr(a.k + w.b * a.k_b + (int64_t)w.hkv * a.k_h);
+  const char *vb = uniform_ptr(a.v + w.b * a.v_b + (int64_t)w.hkv * a.v_h);
+  auto load_tile = [&](int it) {
+    const int j0 = keys.first(it, KT), nv = keys.end(it) - j0;
+    Tl::template fill<KT, 1, false>(kb + (int64_t)j0 * a.k_t, (uint32_t)a.k_t, nv, at_k, 0, lane);
+    Tl::template fill<KT, 1, false>(vb + (int64_t)j0 * a.v_t, (uint32_t)a.v_t, nv, at_v, 0, lane);
+  };
+  if (wave < n_tiles) load_tile(wave);
+  Operand<T> qf[KS], df[KS];
+  float lse2, delta;
+  load_query<T, D>(a, w.b, hq, myq, nq, g, qf, df, lse2, delta);
+  if (wave == 0 && myq < nq && g == 0) a.delta[((int64_t)w.b * a.Hq + hq) * a.Tq + myq] = delta;
+  const float c = a.scale * kLog2e;
+  f32x16 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) o[i] = f32x16{0.f};
+  const Fragments<T, D> fr(at_k, at_k, lane);
+  for (int it = wave; it < n_tiles; it += kWaves) {
+    wait_vmem<0>();
+    const int j0 = keys.first(it, KT), j1 = keys.end(it);
+    const bool masked = !(j0 + KT <= j1 && j0 + KT - 1 <= off + Q0 && (off + Q0 + 31 - j0 < a.W || j0 + KT <= a.S));
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mma(fr.along(blk, ks, 0), qf[ks], ks == 0 ? f32x16{0.f} : s);
+        dp = mma(fr.along(blk, ks, kTileB), df[ks], ks == 0 ? f32x16{0.f} : dp);
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -lse2)) * (dp[v] - delta);
+      if (masked) {
+        const int last = (t < j1 - 1 ? t : j1 - 1) - j0 - 4 * g, first = t - a.W + 1 - j0 - 4 * g, sink = a.S - j0 - 4 * g;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = 32 * blk + mfma_row(v, 0);
+          s[v] = r <= last && (r >= first || r < sink) ? s[v] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[8 * hf + e];
+        Operand<T> ds;
+        to_operand(x, ds);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) o[i] = mma(fr.across(i, 2 * blk + hf, 0), ds, o[i]);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read
+    if (it + kWaves < n_tiles) load_tile(it + kWaves);
+  }
+  float *mine = reinterpret_cast<float *>(lds + wave * 2 * kTileB);
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mine[(16 * i + v) * 64 + lane] = o[i][v];
+  __syncthreads();
+  if (myq >= nq || wave >= DB) return;
+  float sum[16];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) sum[v] = 0.f;
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) {
+    const float *theirs = reinterpret_cast<const float *>(lds + x * 2 * kTileB) + 16 * wave * 64 + lane;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sum[v] += theirs[v * 64];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    store4<T>(row, wave, i, g, a.scale * sum[4 * i], a.scale * sum[4 * i + 1], a.scale * sum[4 * i + 2], a.scale * sum[4 * i + 3]);
 }
 
 // dk and dv of 128 keys, 32 to a wave (K in registers, V in LDS); the queries that see them, head after head of the group, stream
@@ -1033,6 +1297,18 @@ bool strides_ok(int64_t b, int64_t t, int64_t h, const kvm_window_config *c) {
   return t <= (1 << 23);
 }
 
+// Position tiles of `span` queries, of four heads of a group together (by_head) or of one.
+void tile_queries(WinArgs &a, bool by_head, int span) {
+  a.by_head = by_head;
+  a.span = span;
+  a.tiles = (a.Tq + a.span - 1) / a.span;
+  // blocks of position tiles: 2048 positions, fewer where there would not be eight for every XCD
+  int64_t per = 2048 / a.span;
+  const int64_t units = (int64_t)a.B * a.Hkv;
+  while (per > 1 && units * ((a.tiles + per - 1) / per) < 8 * kXcds) per /= 2;
+  a.per_block = (int32_t)per;
+  a.blocks = (int32_t)((a.tiles + per - 1) / per);
+}
 WinArgs base_args(const kvm_window_config *c, int64_t Tq, int64_t Tk, const int32_t *lens) {
   WinArgs a = {};
   a.lens = lens;
@@ -1041,15 +1317,8 @@ WinArgs base_args(const kvm_window_config *c, int64_t Tq, int64_t Tk, const int3
   a.Tq = (int32_t)Tq; a.Tk = (int32_t)Tk;
   a.W = (int32_t)(c->window < Tk ? c->window : Tk);
   a.S = a.W >= Tk ? 0 : (int32_t)(c->n_sink < Tk ? c->n_sink : Tk);   // (nothing is beyond the window: no sinks needed)
-  a.by_head = a.Hq / a.Hkv % kWaves == 0;
-  a.span = a.by_head ? 32 : 32 * kWaves;
-  a.tiles = (int32_t)((Tq + a.span - 1) / a.span);
-  // blocks of position tiles: 2048 positions, fewer where there would not be eight for every XCD
-  int64_t per = 2048 / a.span;
-  const int64_t units = (int64_t)a.B * a.Hkv;
-  while (per > 1 && units * ((a.tiles + per - 1) / per) < 8 * kXcds) per /= 2;
-  a.per_block = (int32_t)per;
-  a.blocks = (int32_t)((a.tiles + per - 1) / per);
+  const bool by_head = a.Hq / a.Hkv % kWaves == 0;
+  tile_queries(a, by_head, by_head ? 32 : 32 * kWaves);
   return a;
 }
 // Workgroups of the query kernels, all blocks full and a multiple of eight of them; 0: more than a grid holds.
@@ -1087,9 +1356,24 @@ size_t sums_bytes(const WinArgs &a, int d) {
   return a.n_part > 1 ? (size_t)a.B * a.Hkv * a.n_part * 2 * a.Tk * d * sizeof(float) : 0;
 }
 
+// Few workgroups for the device: 32 queries of one head in each instead, its waves sharing the key tiles.  Prompts, us, tiles shared / not
+// (workgroups not shared): 512 tokens, 8 heads 9 / 20 (32); 1000, 8 on 2 heads 13 / 33 (64); fp32, 777, 6 on 2 heads 12 / 35 (42);
+// 2048, 16 heads 55 / 66 (256); 1000, 32 on 8 heads, four to a workgroup, 28 / 26 (256); 4096, 16 on 4 heads 73 / 50 (512).
+bool split_tiles(WinArgs &a) {
+  const unsigned grid = query_grid(a);
+  if (grid == 0 || grid >= (a.by_head ? 256u : 512u)) return false;
+  tile_queries(a, false, 32);
+  return true;
+}
 template <typename T, int D>
-hipError_t run_prefill(const WinArgs &a, unsigned grid, hipStream_t st) {
-  static OncePerDevice<hipError_t> once;
+hipError_t run_prefill(const WinArgs &a, unsigned grid, bool split, hipStream_t st) {
+  static OncePerDevice<hipError_t> once, once_split;
+  if (split) {
+    const hipError_t e = allow_lds(once_split, (const void *)window_prefill_split_kernel<T, D>, split_lds<T, D>());
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((window_prefill_split_kernel<T, D>), dim3(grid), dim3(256), (split_lds<T, D>()), st, a);
+    return hipGetLastError();
+  }
   constexpr size_t bytes = 4 * (size_t)kPromptRows<T, D> * D * sizeof(T);
   hipError_t e = allow_lds(once, (const void *)window_prefill_kernel<T, D>, bytes);
   if (e != hipSuccess) return e;
@@ -1097,14 +1381,16 @@ hipError_t run_prefill(const WinArgs &a, unsigned grid, hipStream_t st) {
   return hipGetLastError();
 }
 template <typename T, int D>
-hipError_t run_backward_as(const WinArgs &a, unsigned grid, unsigned units8, hipStream_t st) {
-  static OncePerDevice<hipError_t> once_q, once_kv, once_far;
+hipError_t run_backward_as(const WinArgs &a, unsigned grid, bool split, unsigned units8, hipStream_t st) {
+  static OncePerDevice<hipError_t> once_q, once_split, once_kv, once_far;
   constexpr size_t bytes = 4 * (size_t)kTileRows<T, D> * D * sizeof(T), bytes_kv = kv_lds<T, D>();
-  hipError_t e = allow_lds(once_q, (const void *)window_dq_kernel<T, D>, bytes);
+  hipError_t e = split ? allow_lds(once_split, (const void *)window_dq_split_kernel<T, D>, split_lds<T, D>())
+                       : allow_lds(once_q, (const void *)window_dq_kernel<T, D>, bytes);
   if (e == hipSuccess) e = allow_lds(once_kv, (const void *)window_dkv_kernel<T, D, false>, bytes_kv);
   if (e == hipSuccess && a.n_split > 0) e = allow_lds(once_far, (const void *)window_dkv_kernel<T, D, true>, bytes_kv);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
+  if (split) hipLaunchKernelGGL((window_dq_split_kernel<T, D>), dim3(grid), dim3(256), (split_lds<T, D>()), st, a);
+  else hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((window_dkv_kernel<T, D, false>), dim3(units8 * a.key_tiles * a.n_part), dim3(256), bytes_kv, st, a);
@@ -1180,9 +1466,10 @@ extern "C" int kvm_window_prefill(const kvm_window_config *cfg, const void *q, c
   a.v_b = s.v_b * es; a.v_t = s.v_t * es; a.v_h = s.v_h * es;
   a.o_b = s.o_b * es; a.o_t = s.o_t * es; a.o_h = s.o_h * es;
   a.l_b = s.lse_b; a.l_t = s.lse_t; a.l_h = s.lse_h;
+  const bool split = split_tiles(a);
   const unsigned grid = query_grid(a);
   if (grid == 0) return KVM_ERR_ARG;
-  const hipError_t e = KVM_BY_TYPE(cfg, run_prefill, a, grid, (hipStream_t)stream);
+  const hipError_t e = KVM_BY_TYPE(cfg, run_prefill, a, grid, split, (hipStream_t)stream);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_prefill");
 }
 
@@ -1219,10 +1506,11 @@ extern "C" int kvm_window_backward(const kvm_window_config *cfg, const void *q, 
   a.delta = (float *)workspace;
   a.part = (float *)((char *)workspace + delta_bytes(a));
   a.sums = (float *)((char *)a.part + part_bytes(a, (int)d));
+  const bool split = split_tiles(a);
   const unsigned grid = query_grid(a);
   const int64_t units8 = ((int64_t)a.B * a.Hkv + kXcds - 1) / kXcds * kXcds;
   if (grid == 0 || units8 * a.key_tiles >= (1ll << 31) || (int64_t)a.B * a.Hkv > 65535) return KVM_ERR_ARG;
-  const hipError_t e = KVM_BY_TYPE(cfg, run_backward_as, a, grid, (unsigned)units8, (hipStream_t)stream);
+  const hipError_t e = KVM_BY_TYPE(cfg, run_backward_as, a, grid, split, (unsigned)units8, (hipStream_t)stream);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_backward");
 }
 

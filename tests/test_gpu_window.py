@@ -365,3 +365,33 @@ def test_gradients_of_gradients_are_refused_and_a_graph_can_be_used_twice():
         torch.autograd.grad(out, leaves, x["dout"], retain_graph=True, create_graph=True)
     for a, b in zip(first, torch.autograd.grad(out, leaves, x["dout"])):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("io,d,B,Hq,Hkv,T", [
+    ("bf16", 128, 132, 4, 4, 150), ("bf16", 64, 70, 8, 2, 140), ("bf16", 128, 70, 8, 2, 140),   # a head or four to a workgroup
+    ("f32", 64, 132, 4, 4, 150), ("f32", 128, 132, 4, 4, 140), ("f32", 128, 70, 8, 2, 140)])
+def test_many_sequences(io, d, B, Hq, Hkv, T):
+    """Calls that fill the device: workgroups whose waves share tiles of keys (prompt, dq) and take a key tile's queries whole (dk, dv).
+    Lengths of all kinds, a few of the sequences compared."""
+    import paper_2605_09877_amd as kvm
+    x = make(io, B, T, T, Hq, Hkv, d)
+    lens = [(7 * b) % (T + 1) for b in range(B)]
+    lens[0], lens[B // 2], lens[B - 1] = T, 129, 33
+    W, S = 45, 3
+    kw = dict(window=W, n_sink=S, lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    leaves = [x[n].clone().requires_grad_() for n in "qkv"]
+    o = kvm.kvm_window_attention(*leaves, **kw)
+    grads = torch.autograd.grad(o, leaves, x["dout"])
+    for b in (0, B // 2, B - 1):
+        one = {n: t[b:b + 1] for n, t in x.items()}
+        y = {n: f64(t) for n, t in one.items()}
+        ref = mo.window(y["q"], y["k"], y["v"], W, S, [lens[b]])[0]
+        within(o[b:b + 1], ref, out_bound(io, one, ref, W, S, [lens[b]], None), f"out {b}")
+        rg = mo.window_backward(y["q"], y["k"], y["v"], y["dout"], W, S, [lens[b]])
+        mg = mo.window_backward(y["q"], y["k"], y["v"], y["dout"], W, S, [lens[b]], absolute=True)
+        e = noise(one, None, T * (Hq // Hkv)) + (2 * 2.0 ** -8 + 2.0 ** -14 if io == "bf16" else 0)
+        for got, r, m, name in zip(grads, rg, mg, ("dq", "dk", "dv")):
+            within(got[b:b + 1], r, e * m + (2.0 ** -8 * np.abs(r) if io == "bf16" else 0), f"{name} {b}")
+    for b, n in enumerate(lens):
+        for t in (o, *grads):
+            assert torch.count_nonzero(t[b, n:]) == 0

@@ -361,7 +361,8 @@ int kvm_prepare_qkv(const kvm_prep_params *p, const void *q_raw, const void *k_r
  * in pieces with the keys before it.  lens: nullable device int32 [B], the keys of each sequence of a padded batch (taken as
  * 0 .. Tk): keys behind are not looked at, queries behind get zeros and lse = -infinity.  In out, values that are not finite
  * reach the queries that see them and no others; a query all of whose logits are -infinity gets zeros.  In gradients they
- * also reach keys and queries of the same tiles (up to 128 positions).  Pointers are 16-byte aligned (lse: 4); outputs must not overlap inputs. */
+ * also reach keys and queries of the same tiles (up to 128 positions).  Pointers are 16-byte aligned (lse: 4); outputs must
+ * not overlap inputs. */
 #define KVM_WINDOW_MAX_SINK 128
 typedef struct kvm_window_config {
   int32_t batch, n_q_heads, n_kv_heads, head_dim; /* d: 64 or 128; batch * n_q_heads < 2^24 */
@@ -371,9 +372,9 @@ typedef struct kvm_window_config {
   float scale;                                     /* 0 selects 1 / sqrt(d) */
 } kvm_window_config;
 
-/* Strides as in kvm_prefill_chunked (NULL = dense; gate strides are not looked at), token strides up to 2^23 elements.  lse: [B, Tq, H_q] fp32 natural-log sum of
- * exponentials, or NULL; out_rest: what rounding out to bf16 left of it, rounded to bf16, in out's shape and strides (for
- * kvm_window_backward), or NULL; not written with KVM_F32. */
+/* Strides as in kvm_prefill_chunked (NULL = dense; gate strides are not looked at), token strides up to 2^23 elements;
+ * Tk < 2^30.  lse: [B, Tq, H_q] fp32 natural-log sum of exponentials, or NULL; out_rest: what rounding out to bf16 left of
+ * it, rounded to bf16, in out's shape and strides (for kvm_window_backward), or NULL; not written with KVM_F32. */
 int kvm_window_prefill(const kvm_window_config *cfg, const void *q, const void *k, const void *v, const int32_t *lens,
                        void *out, void *out_rest, float *lse, int64_t Tq, int64_t Tk, const kvm_strides *strides,
                        void *stream);
@@ -405,9 +406,9 @@ int kvm_window_decode(const kvm_window_config *cfg, void *cache_k, void *cache_v
  *   S_t = exp(a_h) S_{t-1} + k_t v_t^T,   out_t = scale * q_t S_t,
  * a_h = log_decay[h] <= 0 a constant of the KV head (device fp32 [H_kv]; it gets no gradient; values above 0 are not
  * refused, the state then grows).  The H_q / H_kv query heads of a group share one state.  Sums and states are
- * fp32; q, k, v, out are KVM_F32 or KVM_BF16.  In prompts tokens are taken 64 at a time (fp32: 32): a NaN or an infinity of a later
- * token's k or v, or an earlier one's, makes NaN of outputs of the same group of tokens; behind it the state is NaN where
- * the recurrence makes it infinite or NaN.
+ * fp32; q, k, v, out are KVM_F32 or KVM_BF16.  In prompts tokens are taken 64 at a time (fp32: 32): a NaN or an infinity
+ * of a later token's k or v, or an earlier one's, makes NaN of outputs of the same group of tokens; behind it the state is
+ * NaN where the recurrence makes it infinite or NaN.
  * lens: nullable device int32 [B], the tokens of each sequence of a padded batch (taken as 0 .. T): rows behind are
  * not looked at, their out is zero, and the state is the one at the sequence's own end.  Every pointer is 16-byte aligned;
  * outputs must not overlap inputs, except that state_out may be state_in itself. */
@@ -418,12 +419,12 @@ typedef struct kvm_linear_config {
 } kvm_linear_config;
 
 /* Bytes of device workspace that kvm_linear_prefill and kvm_linear_backward need for T tokens (start states of the
- * parts a sequence is cut into); 0 on bad arguments. */
+ * parts a sequence is cut into); 0 on bad arguments, which T >= 2^29 is one of, here and below. */
 size_t kvm_linear_workspace_bytes(const kvm_linear_config *cfg, int64_t T);
 
 /* T tokens of every sequence.  q, out: [B, T, H_q, d]; k, v: [B, T, H_kv, d], strided as in kvm_prefill_chunked (NULL =
- * dense; multiples of 16 bytes, token strides up to 2^23 elements; gate and lse strides are not looked at); state_in, state_out: fp32 [B, H_kv, d, d] or NULL (zero; not
- * wanted).  Work is enqueued on `stream`.  Errors: KVM_ERR_ARG, KVM_ERR_CAPACITY (workspace), KVM_ERR_HIP. */
+ * dense; multiples of 16 bytes, token strides up to 2^23 elements; gate and lse strides are not looked at); state_in,
+ * state_out: fp32 [B, H_kv, d, d] or NULL (zero; not wanted).  Work is enqueued on `stream`.  Errors: KVM_ERR_ARG, KVM_ERR_CAPACITY (workspace), KVM_ERR_HIP. */
 int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, const void *k, const void *v, const float *log_decay,
                        const float *state_in, const int32_t *lens, void *out, float *state_out, int64_t T,
                        const kvm_strides *strides, void *workspace, size_t workspace_bytes, void *stream);

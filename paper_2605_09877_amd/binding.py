@@ -657,13 +657,18 @@ def _row_strides(q, k, v, out, lse=None) -> kvm_strides:
                        *((0, 0, 0) if lse is None else lse.stride()))
 
 
+def _number(scale) -> Optional[float]:
+    """A scale as a key of the configurations kept below: the value, also where it is given as a tensor."""
+    return scale if scale is None else float(scale)
+
+
 @functools.lru_cache(maxsize=4096)
 def _linear_config_of(B: int, Hq: int, Hkv: int, d: int, io: int, scale: Optional[float]) -> kvm_linear_config:
-    return kvm_linear_config(B, Hq, Hkv, d, io, 0.0 if scale is None else float(scale))
+    return kvm_linear_config(B, Hq, Hkv, d, io, 0.0 if scale is None else scale)
 
 
 def _linear_config(q, k, scale) -> kvm_linear_config:
-    return _linear_config_of(q.shape[0], *_heads(q, k, 4), _io_of(q), scale)
+    return _linear_config_of(q.shape[0], *_heads(q, k, 4), _io_of(q), _number(scale))
 
 
 def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional[float] = None, out=None, state_out=None,
@@ -733,7 +738,7 @@ def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, a
     active int32 [B] or None: a sequence whose entry is 0 keeps its state and gets zeros."""
     Hq, Hkv, d = _heads(q, k, 3)
     B, dev, dt = q.shape[0], q.device, q.dtype
-    cfg = _linear_config_of(B, Hq, Hkv, d, _io_of(q), scale)
+    cfg = _linear_config_of(B, Hq, Hkv, d, _io_of(q), _number(scale))
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     ptrs = (_want(state, (B, Hkv, d, d), torch.float32, dev, "state"), _want(q, (B, Hq, d), dt, dev, "q"),
@@ -755,7 +760,7 @@ def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, a
 def _window_config(B: int, Hq: int, Hkv: int, d: int, io: int, window: int, n_sink: int, scale) -> kvm_window_config:
     if not 1 <= int(window) < 1 << 30 or not 0 <= int(n_sink) <= KVM_WINDOW_MAX_SINK:
         raise ValueError(f"window: want 1 .. 2^30 - 1, n_sink 0 .. {KVM_WINDOW_MAX_SINK}, got {window} and {n_sink}")
-    return kvm_window_config(B, Hq, Hkv, d, io, int(n_sink), int(window), 0.0 if scale is None else float(scale))
+    return kvm_window_config(B, Hq, Hkv, d, io, int(n_sink), int(window), 0.0 if scale is None else scale)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -778,7 +783,7 @@ def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: O
     B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
     if not 0 < Tq <= Tk:
         raise ValueError(f"q and k: want 0 < Tq <= Tk, got {Tq} and {Tk}")
-    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
+    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, _number(scale))
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     lse = torch.empty((B, Tq, Hq), dtype=torch.float32, device=dev) if want_lse else None
@@ -800,7 +805,7 @@ def window_backward(q, k, v, out, lse, dout, *, window: int, n_sink: int = 0, le
     lib = load_library()
     Hq, Hkv, d = _heads(q, k, 4)
     B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
-    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
+    cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, _number(scale))
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     ptrs = [_want(q, q.shape, q.dtype, dev, "q"), _want(k, (B, Tk, Hkv, d), q.dtype, dev, "k"),
             _want(v, (B, Tk, Hkv, d), q.dtype, dev, "v"), _want(lens, (B,), torch.int32, dev, "lens"),
@@ -848,7 +853,7 @@ def window_decode(cache_k, cache_v, q, k, v, pos, *, window: int, n_sink: int = 
     attended.  q [B,Hq,d]; k, v [B,Hkv,d]."""
     Hq, Hkv, d = _heads(q, k, 3)
     B, dev, dt = q.shape[0], q.device, q.dtype
-    cfg, nbytes = _window_token_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, scale)
+    cfg, nbytes = _window_token_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, _number(scale))
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     rows = (B, Hkv, n_sink + window, d)

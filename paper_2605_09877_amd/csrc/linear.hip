@@ -43,6 +43,7 @@ struct LinArgs {
   int32_t transposed;    // start and seg are [z channel][y channel]
   int32_t fine_state;    // the state is a result
   int32_t T, H, G, units, n_seg, seg_tokens, seg_of_unit, seg_step;
+  int32_t head_parts;    // workgroups that share the heads of x, each with the state of its own
 };
 
 template <typename T>
@@ -91,7 +92,8 @@ __global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(L
   const bool transposed = kPair ? second : a.transposed != 0;
   // the lane's z channel of its wave's 32: such that results, which have z channels as rows, are in natural order
   const int zl = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
-  const int u = blockIdx.x % a.units, seg = blockIdx.x / a.units;
+  const int u = blockIdx.x % a.units, seg_part = blockIdx.x / a.units;
+  const int seg = kMany ? seg_part : seg_part / a.head_parts, part = kMany ? 0 : seg_part % a.head_parts;
   const int b = u / a.H, h = u % a.H;
   int n = a.T;
   if (a.lens) {
@@ -101,17 +103,18 @@ __global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(L
   n = __builtin_amdgcn_readfirstlane(n);
   const int s0 = seg * a.seg_tokens;
   const int s1 = s0 + a.seg_tokens < n ? s0 + a.seg_tokens : n;   // positions s0 .. s1 - 1 of the walk
-  const int heads_x = kMany ? 1 : a.G, heads_y = kMany ? a.G : 1;
+  const int heads_x = kMany ? 1 : a.G / a.head_parts, heads_y = kMany ? a.G : 1;
+  const int head0 = kMany ? h : h * a.G + part * heads_x;   // first head of x
+  const int steps = kMany ? heads_y : kOut ? heads_x : 1;   // of a chunk
   if constexpr (kOut) {   // rows behind the sequence
     const int z0 = s0 > n ? s0 : n, z1 = s0 + a.seg_tokens < a.T ? s0 + a.seg_tokens : a.T;
     constexpr int kParts = Tl::kRowB / 16;
-    for (int i = 64 * wave + lane; i < (z1 - z0) * heads_x * kParts; i += 64 * NW) {
-      const int part = i % kParts, hx = i / kParts % heads_x, t = z0 + i / (kParts * heads_x);
-      *reinterpret_cast<uint4 *>((second ? a.out2 : a.out) + b * a.o_b + (int64_t)t * a.o_t + (int64_t)(h * heads_x + hx) * a.o_h + 16 * part) =
-          make_uint4(0, 0, 0, 0);
-    }
+    for (int t = z0 + (64 * wave + lane) / kParts; t < z1; t += 64 * NW / kParts)
+      for (int hx = 0; hx < heads_x; ++hx)
+        *reinterpret_cast<uint4 *>((second ? a.out2 : a.out) + b * a.o_b + (int64_t)t * a.o_t + (int64_t)(head0 + hx) * a.o_h +
+                                   16 * (lane % kParts)) = make_uint4(0, 0, 0, 0);
   }
-  const bool ends = kOut && a.end && !second && (n > 0 ? s0 < n && n <= s0 + a.seg_tokens : seg == 0);
+  const bool ends = kOut && a.end && !second && part == 0 && (n > 0 ? s0 < n && n <= s0 + a.seg_tokens : seg == 0);
   if (s0 >= n && !(kOut && a.end && n == 0 && seg == 0)) return;   // (an empty sequence's state is passed on)
   if (!kOut && s1 - s0 < a.seg_tokens) return;   // (a segment that another one follows is full)
 
@@ -145,10 +148,10 @@ __global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(L
       }
   }
 
-  const char *xb = uniform_ptr((second ? a.x2 : a.x) + b * a.x_b + (int64_t)(h * heads_x) * a.x_h);
+  const char *xb = uniform_ptr((second ? a.x2 : a.x) + b * a.x_b + (int64_t)head0 * a.x_h);
   const char *yb = uniform_ptr(a.y + b * a.y_b + (int64_t)(h * heads_y) * a.y_h);
   const char *zb = uniform_ptr(a.z + b * a.z_b + (int64_t)(h * heads_y) * a.z_h);
-  char *ob = (second ? a.out2 : a.out) + b * a.o_b + (int64_t)(h * heads_x) * a.o_h;
+  char *ob = (second ? a.out2 : a.out) + b * a.o_b + (int64_t)head0 * a.o_h;
   // first row in memory of the chunk at position c0 with nv tokens
   auto first_row = [&](int c0, int nv) { return kRev ? n - c0 - nv : c0; };
   auto load_yz = [&](int c0, int hd, uint32_t buf) {
@@ -200,10 +203,9 @@ __global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(L
   }
   for (int c0 = s0; c0 < s1; c0 += C) {
     const int nv = s1 - c0 < C ? s1 - c0 : C;
-    for (int hd = 0; hd < a.G; ++hd) {
-      if (!kOut && !kMany && hd > 0) break;
+    for (int hd = 0; hd < steps; ++hd) {
       const bool new_x = kMany ? hd == 0 : true, new_yz = kMany ? true : hd == 0;
-      const bool last = hd == a.G - 1 || (!kOut && !kMany);
+      const bool last = hd == steps - 1;
       const uint32_t y_along = here(at_y + buf * kTileB + lane_along), y_across = here(at_y + buf * kTileB + lane_across);
       // this step's tiles: asked for ahead of the stores of the step before, which need not have ended (a lane stores
       // kStores times for a full chunk)
@@ -500,9 +502,21 @@ bool valid(const kvm_linear_config *c) {
 }
 float scale_of(const kvm_linear_config *c) { return c->scale > 0.f ? c->scale : 1.f / sqrtf((float)c->head_dim); }
 
+constexpr int64_t kMaxTokens = 1ll << 29;   // the end of twice a segment is a 32-bit position
+
 // Segments a sequence is cut into: one workgroup has one segment of one unit, and the device holds `fill` of them at once.  The
-// first pass reads y and z once more, so there are no more than it takes to fill the device; a segment has two chunks at
-// least, and sequences of fewer than eight chunks are not cut (two more launches cost more than the chunks walked less).
+// first pass reads y and z once more, so there are no more than it takes to fill the device.  Up to 32 segments may be a chunk each,
+// more have two chunks at least (every segment is one more state to add up), and short sequences are not cut: two more launches cost
+// more than the chunks walked less.  Prompts of 8 heads of 128 channels (in brackets their gradients), us, by the chunks of a segment:
+//             one         two         four        not cut
+//   bf16  5   32 (57)     36 (57)     38 (63)     23 (45)
+//         8   34 (60)     37 (71)     47 (86)     33 (68)
+//        16   40 (70)     40 (75)     48 (101)    62 (129)
+//        32   46 (84)     45 (87)     50 (106)    120 (251)
+//        64   55 (105)    48 (92)     53 (111)    235 (496)
+//   fp32  5   37 (81)     46 (105)    49 (123)    42 (110)
+//         8   39 (85)     47 (119)    66 (182)    65 (172)
+//        32   50 (107)    55 (136)    70 (203)    245 (665)
 struct Cut {
   int n_seg, seg_tokens;
 };
@@ -511,8 +525,9 @@ Cut cut_of(const kvm_linear_config *c, int64_t T) {
   const int64_t units = (int64_t)c->batch * c->n_kv_heads, chunks = (T + chunk - 1) / chunk;
   const int64_t fill = c->head_dim == 128 ? 512 : 1024;
   int64_t n = (fill + units - 1) / units;
-  if (n > chunks / 2) n = chunks / 2;
-  if (n < 1 || chunks < 8) n = 1;
+  const int64_t most = chunks <= 32 ? chunks : chunks / 2 > 32 ? chunks / 2 : 32;
+  if (n > most) n = most;
+  if (n < 1 || chunks < (c->io_dtype == KVM_BF16 ? 8 : 5)) n = 1;
   const int64_t per = (chunks + n - 1) / n;
   return Cut{(int)((chunks + per - 1) / per), (int)(per * chunk)};
 }
@@ -529,11 +544,22 @@ hipError_t launch_walk_as(const LinArgs &a, int n_wg, hipStream_t st) {
   hipLaunchKernelGGL((linear_walk_kernel<T, D, kRev, kMany, kOut, kPair, kFine>), dim3((unsigned)n_wg), dim3(kPair ? 4 * D : 2 * D), bytes, st, a);
   return hipGetLastError();
 }
+// Few workgroups for the device: the query heads of a group are shared among several, up to one each, that walk the same state
+// (1000 tokens of 32 heads on 8: 43 us, 50 with the heads of a group in one workgroup).
+int head_parts_of(const kvm_linear_config *c, int n_wg) {
+  const int G = c->n_q_heads / c->n_kv_heads, most = (c->head_dim == 128 ? 512 : 1024) / n_wg;
+  int parts = 1;
+  for (int k = 2; k <= G && k <= most; ++k)
+    if (G % k == 0) parts = k;
+  return parts;
+}
 // Prompts of up to kFineTokens tokens are a few chunks long and wait for latencies: two more operands for each product cost
 // them nothing that shows.  Longer ones have many pairs behind most outputs, and the roundings of these average out.
 constexpr int kFineTokens = 128;
 template <bool kRev, bool kMany, bool kOut, bool kPair>
-hipError_t launch_walk(const kvm_linear_config *c, const LinArgs &a, int n_wg, hipStream_t st) {
+hipError_t launch_walk(const kvm_linear_config *c, LinArgs a, int n_wg, hipStream_t st) {
+  a.head_parts = kOut && !kMany ? head_parts_of(c, n_wg) : 1;
+  n_wg *= kMany ? 1 : a.head_parts;
   if (c->io_dtype == KVM_F32)
     return c->head_dim == 128 ? launch_walk_as<float, 128, kRev, kMany, kOut, kPair, false>(a, n_wg, st)
                               : launch_walk_as<float, 64, kRev, kMany, kOut, kPair, false>(a, n_wg, st);
@@ -573,7 +599,7 @@ void launch_token_as(const LinTokenArgs &a, int units, hipStream_t st) {
 }  // namespace kvm
 
 extern "C" size_t kvm_linear_workspace_bytes(const kvm_linear_config *cfg, int64_t T) {
-  if (!kvm::valid(cfg) || T <= 0 || T >= (1ll << 31)) return 0;
+  if (!kvm::valid(cfg) || T <= 0 || T >= kvm::kMaxTokens) return 0;
   const kvm::Cut cut = kvm::cut_of(cfg, T);
   return cut.n_seg > 1 ? cut.n_seg * kvm::state_bytes(cfg) : 256;
 }
@@ -583,7 +609,7 @@ extern "C" int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, c
                                   float *state_out, int64_t T, const kvm_strides *strides, void *workspace,
                                   size_t workspace_bytes, void *stream) {
   using namespace kvm;
-  if (!valid(cfg) || T <= 0 || T >= (1ll << 31) || !q || !k || !v || !log_decay || !out || !workspace) return KVM_ERR_ARG;
+  if (!valid(cfg) || T <= 0 || T >= kMaxTokens || !q || !k || !v || !log_decay || !out || !workspace) return KVM_ERR_ARG;
   if (!al16(q) || !al16(k) || !al16(v) || !al16(out) || !al16(state_in) || !al16(state_out) || !al16(workspace)) return KVM_ERR_ARG;
   if (workspace_bytes < kvm_linear_workspace_bytes(cfg, T)) return KVM_ERR_CAPACITY;
   const int64_t d = cfg->head_dim, hq = cfg->n_q_heads, hk = cfg->n_kv_heads, es = cfg->io_dtype == KVM_BF16 ? 2 : 4;
@@ -622,7 +648,7 @@ extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, 
                                    const float *dstate_out, void *dq, void *dk, void *dv, float *dstate_in, int64_t T,
                                    const void *kept, void *workspace, size_t workspace_bytes, void *stream) {
   using namespace kvm;
-  if (!valid(cfg) || T <= 0 || T >= (1ll << 31) || !q || !k || !v || !log_decay || !dout || !dq || !dk || !dv || !workspace)
+  if (!valid(cfg) || T <= 0 || T >= kMaxTokens || !q || !k || !v || !log_decay || !dout || !dq || !dk || !dv || !workspace)
     return KVM_ERR_ARG;
   const void *ptrs[] = {q, k, v, state_in, dout, dstate_out, dq, dk, dv, dstate_in, kept, workspace};
   for (const void *x : ptrs)

@@ -292,3 +292,51 @@ def test_gradients_of_gradients_are_refused_and_a_graph_can_be_used_twice():
         torch.autograd.grad(out, leaves, x["dout"], retain_graph=True, create_graph=True)
     for a, b in zip(first, torch.autograd.grad(out, leaves, x["dout"])):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("io,d,B,Hq,Hkv", [("bf16", 128, 140, 8, 4), ("bf16", 64, 140, 4, 2), ("f32", 128, 140, 4, 4)])
+def test_many_sequences(io, d, B, Hq, Hkv):
+    """Units enough to fill the device without cutting sequences or sharing heads; a few of the sequences compared."""
+    import paper_2605_09877_amd as kvm
+    T = 330
+    x = make(io, B, T, Hq, Hkv, d, slow=10.0)
+    lens = [(11 * b) % (T + 1) for b in range(B)]
+    lens[0], lens[B // 2], lens[B - 1] = T, 129, 64
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    leaves = [x[n].clone().requires_grad_() for n in ("q", "k", "v", "state")]
+    out, st = kvm.kvm_linear_attention(*leaves[:3], x["log_decay"], state=leaves[3], lens=dl)
+    grads = torch.autograd.grad((out, st), leaves, (x["dout"], x["dstate"]))
+    ld = f64(x["log_decay"])
+    for b in (0, B // 2, B - 1):
+        one = {n: t if n == "log_decay" else t[b:b + 1] for n, t in x.items()}
+        y = {n: f64(t) for n, t in one.items()}
+        ref = (*mo.linear(y["q"], y["k"], y["v"], ld, y["state"], [lens[b]]),
+               *mo.linear_backward(y["q"], y["k"], y["v"], ld, y["dout"], y["state"], y["dstate"], [lens[b]]))
+        mag = magnitudes(one, [lens[b]], None)
+        for i, (got, name) in enumerate(zip((out, st, *grads), ("out", "state", "dq", "dk", "dv", "dstate"))):
+            check("f32" if name in ("state", "dstate") else io, got[b:b + 1], ref[i], mag[i], d, T, f"{name} {b}")
+
+
+@pytest.mark.parametrize("io,G", [("bf16", 6), ("f32", 4), ("bf16", 7)])
+def test_heads_shared_among_workgroups_and_single_chunk_segments(io, G):
+    """One unit, many query heads: as many workgroups as divide the group walk its state, each cut chunk by chunk."""
+    run_case(io, 1, 64 * 9 + 5 if io == "bf16" else 32 * 7 + 3, G, 1, 128, slow=9.0)
+
+
+def test_backward_with_and_without_what_the_prompt_kept():
+    import paper_2605_09877_amd as kvm
+    x = make("bf16", 1, 1500, 2, 1, 128)
+    keep = []
+    kvm.linear_prefill(x["q"], x["k"], x["v"], x["log_decay"], state=x["state"], keep=keep)
+    held = keep[0].clone()
+    args = (x["q"], x["k"], x["v"], x["log_decay"], x["dout"])
+    a = kvm.linear_backward(*args, state=x["state"], kept=keep[0], want_dstate=True)
+    b = kvm.linear_backward(*args, state=x["state"], want_dstate=True)
+    assert torch.equal(keep[0], held)   # read alone
+    # (without it the states that dq starts from are made of 16 bits of every decayed value, not of 24)
+    for p, q in zip(a[1:], b[1:]):
+        assert torch.equal(p, q)
+    mag = magnitudes({n: t for n, t in x.items() if n != "dstate"} | {"dstate": None}, None, None)[2]
+    assert np.all(np.abs(f64(a[0]) - f64(b[0])) <= 2.0 ** -7 * np.abs(f64(a[0])) + 2.0 ** -14 * mag)
+    with pytest.raises(ValueError):
+        kvm.linear_backward(*args, kept=keep[0][:-256])

@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(L
                                    16 * (lane % kParts)) = make_uint4(0, 0, 0, 0);
   }
   const bool ends = kOut && a.end && !second && part == 0 && (n > 0 ? s0 < n && n <= s0 + a.seg_tokens : seg == 0);
-  if (s0 >= n && !(kOut && a.end && n == 0 && seg == 0)) return;   // (an empty sequence's state is passed on)
+  if (s0 >= n && !(ends && n == 0)) return;   // (an empty sequence's state is passed on)
   if (!kOut && s1 - s0 < a.seg_tokens) return;   // (a segment that another one follows is full)
 
   // ---- powers of the decay
@@ -134,10 +134,12 @@ __global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(L
   // ---- the state: element v of block blk is (y channel 32 blk + 16 (v / 8) + 8 g + v % 8, z channel 32 wave + zl)
   f32x16 S[NB];
   {
-    const float *src = seg == 0 ? a.start : a.seg + ((int64_t)u * a.seg_of_unit + seg * a.seg_step) * (D * D);
-    const float f = seg == 0 ? a.start_scale : 1.f;
+    // (of a sequence that is cut, the first segment's too is in seg: `start` may be `end`, which another workgroup writes)
+    const bool cut = a.seg_of_unit > 1 && n > 0;
+    const float *src = cut ? a.seg + ((int64_t)u * a.seg_of_unit + seg * a.seg_step) * (D * D)
+                           : a.start ? a.start + (int64_t)u * (D * D) : nullptr;
+    const float f = cut ? 1.f : a.start_scale;
     if (!kOut) src = nullptr;
-    else if (seg == 0 && src) src += (int64_t)u * (D * D);
     const int zc = 32 * wave + zl;
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk)
@@ -559,6 +561,7 @@ constexpr int kFineTokens = 128;
 template <bool kRev, bool kMany, bool kOut, bool kPair>
 hipError_t launch_walk(const kvm_linear_config *c, LinArgs a, int n_wg, hipStream_t st) {
   a.head_parts = kOut && !kMany ? head_parts_of(c, n_wg) : 1;
+  if (a.n_seg == 1 && a.start && a.start == a.end) a.head_parts = 1;   // (one workgroup reads the state before it writes it)
   n_wg *= kMany ? 1 : a.head_parts;
   if (c->io_dtype == KVM_F32)
     return c->head_dim == 128 ? launch_walk_as<float, 128, kRev, kMany, kOut, kPair, false>(a, n_wg, st)
@@ -660,6 +663,7 @@ extern "C" int kvm_linear_backward(const kvm_linear_config *cfg, const void *q, 
   hipStream_t st = (hipStream_t)stream;
   hipError_t e = hipSuccess;
   if (hq * d > (1 << 23)) return KVM_ERR_ARG;
+  if (cfg->batch * hk * 4 * d >= 1ll << 32) return KVM_ERR_ARG;   // more threads than a launch has
   LinArgs c = {};
   c.log_decay = log_decay; c.lens = lens; c.seg = (float *)workspace; c.scale = scale;
   c.T = (int32_t)T; c.H = (int32_t)hk; c.G = (int32_t)(hq / hk); c.units = cfg->batch * cfg->n_kv_heads;

@@ -340,3 +340,29 @@ def test_backward_with_and_without_what_the_prompt_kept():
     assert np.all(np.abs(f64(a[0]) - f64(b[0])) <= 2.0 ** -7 * np.abs(f64(a[0])) + 2.0 ** -14 * mag)
     with pytest.raises(ValueError):
         kvm.linear_backward(*args, kept=keep[0][:-256])
+
+
+@pytest.mark.parametrize("io,B,T,Hq,Hkv,d", [
+    ("bf16", 1, 130, 8, 1, 128), ("bf16", 2, 4000, 8, 2, 128), ("bf16", 40, 1030, 4, 4, 64), ("f32", 1, 300, 6, 2, 64)])
+def test_state_given_back_in_place(io, B, T, Hq, Hkv, d):
+    """state_out is the state the call starts from: its readers are not the workgroups that write it."""
+    import paper_2605_09877_amd as kvm
+    x = make(io, B, T, Hq, Hkv, d, slow=8.0)
+    lens = torch.tensor([T - (b * 37) % T for b in range(B)], dtype=torch.int32, device=DEV)
+    if B > 1:
+        lens[1] = 0
+    a = (x["q"], x["k"], x["v"], x["log_decay"])
+    out, end = kvm.linear_prefill(*a, state=x["state"], lens=lens)
+    st = x["state"].clone()
+    out2, end2 = kvm.linear_prefill(*a, state=st, lens=lens, state_out=st)
+    assert end2 is st and torch.equal(out, out2) and torch.equal(end, st)
+
+
+def test_scale_by_value():
+    import paper_2605_09877_amd as kvm
+    x = make("f32", 1, 40, 1, 1, 64)
+    a = (x["q"], x["k"], x["v"], x["log_decay"])
+    scale = torch.tensor(0.5)
+    half = kvm.linear_prefill(*a, scale=scale)[0]
+    scale.fill_(0.25)
+    assert torch.equal(half, 2 * kvm.linear_prefill(*a, scale=scale)[0])

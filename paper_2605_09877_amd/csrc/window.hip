@@ -1040,8 +1040,8 @@ __global__ __launch_bounds__(256) void window_sum_kernel(WinArgs a) {
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_sinks_kernel(WinArgs a) {
   __shared__ float sums[4][64];
-  const int u = blockIdx.y, b = u / a.Hkv, hkv = u % a.Hkv, quarter = threadIdx.x / 64;
-  const int i = blockIdx.x * 64 + threadIdx.x % 64;   // (2 S D is a multiple of 64)
+  const int u = blockIdx.x / (2 * a.S * D / 64), b = u / a.Hkv, hkv = u % a.Hkv, quarter = threadIdx.x / 64;
+  const int i = blockIdx.x % (2 * a.S * D / 64) * 64 + threadIdx.x % 64;   // (2 S D is a multiple of 64)
   const int which = i / (a.S * D), key = i / D % a.S, ch = i % D;
   const float *p = a.part + (((int64_t)u * a.parts * 2 + which) * a.sink_rows + key) * D + ch;
   float sum = 0.f;
@@ -1073,9 +1073,10 @@ struct CacheArgs {
 __global__ __launch_bounds__(256) void window_fill_kernel(CacheArgs a, int row_b) {
   const int64_t rows = a.S + a.W;
   const int parts = row_b / 16;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t wgs = (uint32_t)((rows * parts + 255) / 256);   // of a unit
+  const int64_t i = (int64_t)(blockIdx.x % wgs) * 256 + threadIdx.x;
   if (i >= rows * parts) return;
-  const int u = blockIdx.y, b = u / a.Hkv, h = u % a.Hkv, part = (int)(i % parts);
+  const int u = blockIdx.x / wgs, b = u / a.Hkv, h = u % a.Hkv, part = (int)(i % parts);
   const int64_t r = i / parts;
   int64_t n = a.T;
   if (a.at) n = a.at[b] < a.T ? a.at[b] : a.T;
@@ -1280,6 +1281,8 @@ __global__ __launch_bounds__(256) void window_join_kernel(CacheArgs a) {
 
 // ---- host side
 
+constexpr int64_t kMostWgs = 1ll << 24;   // workgroups of 256 threads: a launch has fewer than 2^32
+
 bool valid(const kvm_window_config *c) {
   if (!c || c->batch <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->n_q_heads % c->n_kv_heads) return false;
   if (c->head_dim != 64 && c->head_dim != 128) return false;
@@ -1327,7 +1330,7 @@ WinArgs base_args(const kvm_window_config *c, int64_t Tq, int64_t Tk, const int3
 unsigned query_grid(const WinArgs &a) {
   const int64_t G = a.Hq / a.Hkv, groups = ((int64_t)a.B * a.Hkv * a.blocks + kXcds - 1) / kXcds * kXcds;
   const int64_t n = groups * a.per_block * (a.by_head ? G / kWaves : G);
-  return n < (1ll << 31) ? (unsigned)n : 0;
+  return n < kMostWgs ? (unsigned)n : 0;
 }
 // The queries beyond a sink's window: ranges of one tile of each head for every wave at least, as many as fill the device (two
 // workgroups to a compute unit) and 64 at most.
@@ -1408,8 +1411,7 @@ hipError_t run_backward_as(const WinArgs &a, unsigned grid, bool split, unsigned
     hipLaunchKernelGGL((window_sum_kernel<T, D>), dim3(wgs, (unsigned)(a.B * a.Hkv)), dim3(256), 0, st, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((window_sinks_kernel<T, D>), dim3((unsigned)(2 * a.S * D / 64), (unsigned)(a.B * a.Hkv)), dim3(256), 0,
-                     st, a);
+  hipLaunchKernelGGL((window_sinks_kernel<T, D>), dim3((unsigned)(2 * a.S * D / 64) * (a.B * a.Hkv)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -1511,7 +1513,7 @@ extern "C" int kvm_window_backward(const kvm_window_config *cfg, const void *q, 
   const bool split = split_tiles(a);
   const unsigned grid = query_grid(a);
   const int64_t units8 = ((int64_t)a.B * a.Hkv + kXcds - 1) / kXcds * kXcds;
-  if (grid == 0 || units8 * a.key_tiles >= (1ll << 31) || (int64_t)a.B * a.Hkv > 65535) return KVM_ERR_ARG;
+  if (grid == 0 || units8 * a.key_tiles >= kMostWgs || (int64_t)a.B * a.Hkv * 2 * a.S * d / 64 >= kMostWgs) return KVM_ERR_ARG;
   const hipError_t e = KVM_BY_TYPE(cfg, run_backward_as, a, grid, split, (unsigned)units8, (hipStream_t)stream);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_backward");
 }
@@ -1529,15 +1531,14 @@ extern "C" int kvm_window_fill(const kvm_window_config *cfg, void *cache_k, void
   }
   if (!strides_ok(s.k_b, s.k_t, s.k_h, cfg) || !strides_ok(s.v_b, s.v_t, s.v_h, cfg)) return KVM_ERR_ARG;
   const int64_t units = (int64_t)cfg->batch * hk, parts = d * es / 16;
-  if (units > 65535) return KVM_ERR_ARG;
   CacheArgs a = {};
   a.ck = (char *)cache_k; a.cv = (char *)cache_v; a.k = (const char *)k; a.v = (const char *)v;
   a.k_b = s.k_b * es; a.k_t = s.k_t * es; a.k_h = s.k_h * es;
   a.v_b = s.v_b * es; a.v_t = s.v_t * es; a.v_h = s.v_h * es;
   a.at = lens; a.W = cfg->window; a.S = cfg->n_sink; a.T = (int32_t)T; a.B = cfg->batch; a.Hkv = (int32_t)hk;
   const int64_t wgs = ((a.S + a.W) * parts + 255) / 256;
-  if (wgs >= (1ll << 31)) return KVM_ERR_ARG;
-  hipLaunchKernelGGL(window_fill_kernel, dim3((unsigned)wgs, (unsigned)units), dim3(256), 0, (hipStream_t)stream, a, (int)(d * es));
+  if (wgs * units >= kMostWgs) return KVM_ERR_ARG;
+  hipLaunchKernelGGL(window_fill_kernel, dim3((unsigned)(wgs * units)), dim3(256), 0, (hipStream_t)stream, a, (int)(d * es));
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_fill");
 }
@@ -1566,7 +1567,7 @@ extern "C" int kvm_window_decode(const kvm_window_config *cfg, void *cache_k, vo
   a.W = cfg->window; a.S = cfg->n_sink; a.B = cfg->batch; a.Hq = cfg->n_q_heads; a.Hkv = cfg->n_kv_heads;
   cut_rows(a, cfg);
   const int64_t G = a.Hq / a.Hkv, grid = (int64_t)a.B * a.Hkv * ((G + kHeads - 1) / kHeads) * a.n_split;
-  if (grid >= (1ll << 31)) return KVM_ERR_ARG;
+  if (grid >= kMostWgs) return KVM_ERR_ARG;
   const hipError_t e = KVM_BY_TYPE(cfg, run_token, a, (unsigned)grid, (hipStream_t)stream);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_decode");
 }

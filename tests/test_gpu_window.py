@@ -395,3 +395,35 @@ def test_many_sequences(io, d, B, Hq, Hkv, T):
     for b, n in enumerate(lens):
         for t in (o, *grads):
             assert torch.count_nonzero(t[b, n:]) == 0
+
+
+def test_more_units_than_a_grids_second_dimension():
+    """70000 sequences of a few tokens: gradients with sinks, the cache filled and asked."""
+    import paper_2605_09877_amd as kvm
+    B, T, W, S, d = 70000, 4, 2, 1, 64
+    x = make("bf16", 8, T, T, 1, 1, d)
+    many = {n: t.repeat(B // 8, 1, 1, 1) for n, t in x.items()}
+    leaves = [many[n].clone().requires_grad_() for n in "qkv"]
+    o = kvm.kvm_window_attention(*leaves, window=W, n_sink=S)
+    grads = torch.autograd.grad(o, leaves, many["dout"])
+    ck, cv = kvm.window_cache(B, 1, d, window=W, n_sink=S, device=DEV)
+    kvm.window_fill(ck, cv, many["k"], many["v"], window=W, n_sink=S)
+    for t in (o, *grads, ck, cv):   # the same eight sequences again and again
+        t = t.unflatten(0, (B // 8, 8))
+        assert torch.equal(t, t[:1].expand_as(t))
+    y = {n: f64(t) for n, t in x.items()}
+    ref = mo.window(y["q"], y["k"], y["v"], W, S)[0]
+    within(o[:8], ref, out_bound("bf16", x, ref, W, S, None, None), "out")
+    rg = mo.window_backward(y["q"], y["k"], y["v"], y["dout"], W, S)
+    mg = mo.window_backward(y["q"], y["k"], y["v"], y["dout"], W, S, absolute=True)
+    for got, r, m, name in zip(grads, rg, mg, ("dq", "dk", "dv")):
+        within(got[:8], r, (noise(x, None, T) + 2 * 2.0 ** -8 + 2.0 ** -14) * m + 2.0 ** -8 * np.abs(r), name)
+    assert torch.equal(ck[:8, 0], x["k"][:, [0, 3, 2], 0]) and torch.equal(cv[-8:, 0], x["v"][:, [0, 3, 2], 0])
+    pos = torch.full((B,), T, dtype=torch.int32, device=DEV)   # sees positions 0, 3 and 4
+    t = kvm.window_decode(ck, cv, *(many[n][:, i].contiguous() for i, n in enumerate("qkv")), pos, window=W, n_sink=S)
+    order = dict(k=np.concatenate([y["k"][:, [0, 3]], y["k"][:, 1:2]], 1), v=np.concatenate([y["v"][:, [0, 3]], y["v"][:, 2:3]], 1))
+    ref = mo.window(y["q"][:, :1], order["k"], order["v"], 3)[0]
+    t8 = t.unflatten(0, (B // 8, 8))
+    assert torch.equal(t8, t8[:1].expand_as(t8))
+    one = dict(q=x["q"][:, :1], k=torch.as_tensor(order["k"]), v=torch.as_tensor(order["v"]))
+    within(t[:8, None], ref, out_bound("bf16", one, ref, 3, 0, None, None), "token")

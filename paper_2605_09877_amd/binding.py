@@ -653,8 +653,13 @@ def _heads(q: torch.Tensor, k: torch.Tensor, dims: int):
 
 
 def _row_strides(q, k, v, out, lse=None) -> kvm_strides:
-    return kvm_strides(*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *out.stride()[:3], 0, 0, 0,
-                       *((0, 0, 0) if lse is None else lse.stride()))
+    """Their element strides; an axis of one entry has whatever stride torch left there, and is given one that rows have."""
+    def of(t):
+        stride, shape = t.stride(), t.shape
+        if 1 in shape[:3]:
+            return [n if size > 1 else shape[3] for n, size in zip(stride[:3], shape)]
+        return stride[:3]
+    return kvm_strides(*of(q), *of(k), *of(v), *of(out), 0, 0, 0, *((0, 0, 0) if lse is None else lse.stride()))
 
 
 def _number(scale) -> Optional[float]:

@@ -267,3 +267,13 @@ def test_oracle_gradients_are_slopes():
             h = 1e-5
             slope = ((f(step(h)) - f(step(-h))) * dout).sum() / (2 * h)
             assert abs(slope - (g * way).sum()) <= 1e-7 * (1 + np.abs(g * way).sum())
+
+
+def test_strides_of_axes_of_one_entry():
+    """Such an axis is never stepped along: its stride, which may be anything, is not looked at."""
+    q = torch.empty(64).as_strided((1, 1, 1, 64), (3, 5, 7, 1))
+    k = torch.empty(2, 9, 1, 64).as_strided((2, 9, 1, 64), (9 * 64, 64, 1, 1))
+    s = kb._row_strides(q, k, k, q)
+    assert (s.q_b, s.q_t, s.q_h) == (64, 64, 64) and (s.k_b, s.k_t, s.k_h) == (576, 64, 64) and (s.o_b, s.o_t, s.o_h) == (64, 64, 64)
+    wide = torch.empty(2, 9, 3, 128)[:, :, :, :64]
+    assert (kb._row_strides(wide, k, k, wide).q_t, kb._row_strides(wide, k, k, wide).q_h) == (384, 128)

@@ -427,3 +427,21 @@ def test_more_units_than_a_grids_second_dimension():
     assert torch.equal(t8, t8[:1].expand_as(t8))
     one = dict(q=x["q"][:, :1], k=torch.as_tensor(order["k"]), v=torch.as_tensor(order["v"]))
     within(t[:8, None], ref, out_bound("bf16", one, ref, 3, 0, None, None), "token")
+
+
+@pytest.mark.parametrize("io,d,step", [("bf16", 128, 0.02), ("bf16", 64, 0.5), ("f32", 64, 0.1), ("f32", 128, -0.3)])
+def test_maxima_that_rise_or_fall_along_the_keys(io, d, step):
+    """A logit of about step for every key: the reference of the exponentials moves often, seldom, or never again; in calls of many
+    sequences and of one."""
+    import paper_2605_09877_amd as kvm
+    B, T, W, S = 132, 200, 150, 2
+    x = make(io, 1, T, T, 4, 4, d, seed=3)
+    x["q"] = (1 + 0.1 * x["q"].float()).to(DT[io])
+    x["k"] = (step * d ** -0.5 * torch.arange(T, device=DEV).view(1, T, 1, 1) + 0.05 * x["k"].float()).to(DT[io])
+    y = {n: f64(t) for n, t in x.items()}
+    ref = mo.window(y["q"], y["k"], y["v"], W, S)[0]
+    tol = out_bound(io, x, ref, W, S, None, None)
+    for n in (1, B):
+        out, lse = kvm.window_prefill(*(x[m].repeat(n, 1, 1, 1) for m in "qkv"), window=W, n_sink=S, want_lse=True)
+        within(out[:1], ref, tol, f"out of {n}")
+        assert torch.equal(out, out[:1].expand_as(out)) and torch.equal(lse, lse[:1].expand_as(lse))

@@ -5,6 +5,15 @@
 // of consecutive positions otherwise.  Keys come in tiles, the sinks in front of the window first, then the window of
 // the workgroup's first query up to its last query, under one online softmax (seq_tiles.h for the operands):
 //   S^T[key, query] = K Q^T,  P^T = 2^(S^T scale log2 e - m),  O^T[channel, query] += V^T P^T
+// Gradients, with D = dout . out and dP = dout V^T:  dS = P (dP - D),  dq = scale dS K  (one kernel, a workgroup's queries again),
+// dk = scale dS^T q,  dv = P^T dout  (another, a workgroup's keys): seven products for the five there are, and no atomics.
+// Single token: one pass over the rows that its sequence sees of a ring cache.
+//
+// What they reach (bf16, 128 channels): prompt, 2 sequences of 16k tokens, 32 heads on 8, window 2048: 1065 us, 0.97 PFLOP/s, where a
+// large matrix product of a library takes 1.24.  Matrix instructions are 46 % of the cycles; the vector instructions of a tile (a
+// quarter-rate exponential for every pair) take about as many cycles again, LDS reads and the tiles' direct loads the rest (without
+// either, in a copy made to measure: -10 and -14 %).  Two sequences of 8k tokens, window 1024, of both passes: 411 us forward, 542 dq,
+// 700 dk and dv, 79 the sinks' far queries.  Single token, 64 sequences, 8 KV heads, 4100 rows: 178 us, 5.7 TB/s, the card's read rate.
 #include <math.h>
 
 #include <type_traits>
@@ -45,10 +54,11 @@ struct WinArgs {
   int32_t key_tiles;
 };
 
-template <typename T, int D>
-constexpr int kTileRows = D * (int)sizeof(T) <= 256 ? 64 : 32;   // keys of a tile in the dq kernel: 16 KiB at most
-template <typename T, int D>
-constexpr int kPromptRows = D * (int)sizeof(T) <= 128 ? 64 : 32;   // in the prompt kernel
+// Keys of a tile.  With 32 the prompt kernel has registers for three workgroups to a compute unit, in whose turns the exponentials of one
+// run beside the products of another: 2 sequences of 16k tokens, 32 heads of 128 on 8, window 2048: 1094 us, 1147 with 64 and two
+// workgroups.  Rows of 64 channels, us, 32 / 64: 4 x 4k tokens, 16 heads on 4, 70 / 77; 2k, 16 heads, 15 / 20; 8 x 1000, 8 heads, 24 /
+// 21, the one kind that loses.  dq: 4 x 4k, 16 heads of 64 on 4, with dk and dv 207 / 216.
+constexpr int kTileRows = 32;
 
 __device__ __forceinline__ int tokens_of(const WinArgs &a, int b) {
   int n = a.Tk;
@@ -245,7 +255,7 @@ struct Fragments {
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 1) void window_prefill_kernel(WinArgs a) {
   using Tl = Tile<T, D>;
-  constexpr int KT = kPromptRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr int KT = kTileRows, NB = KT / 32, KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = KT * Tl::kRowB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t at_k = lds_addr_of(lds), at_v = at_k + 2 * kTileB;
@@ -387,12 +397,12 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 1) void window_pref
 // workgroup's loop, which is a quarter as long.
 template <typename T, int D>
 constexpr size_t split_lds() {
-  return kWaves * (2 * (size_t)kPromptRows<T, D> * D * sizeof(T) + 2 * 64 * sizeof(float)) + 32 * sizeof(int);
+  return kWaves * (2 * (size_t)kTileRows * D * sizeof(T) + 2 * 64 * sizeof(float)) + 32 * sizeof(int);
 }
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_prefill_split_kernel(WinArgs a) {
   using Tl = Tile<T, D>;
-  constexpr int KT = kPromptRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr int KT = kTileRows, NB = KT / 32, KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = KT * Tl::kRowB;
   constexpr int kLoads = (int)(kTileB / 1024);   // of a wave for a tile
   static_assert(2 * kTileB >= 64 * 16 * DB * sizeof(float), "a wave's result fits its tiles");
@@ -586,7 +596,7 @@ __device__ __forceinline__ void load_query(const WinArgs &a, int b, int hq, int 
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_kernel(WinArgs a) {
   using Tl = Tile<T, D>;
-  constexpr int KT = kTileRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr int KT = kTileRows, NB = KT / 32, KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = KT * Tl::kRowB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t at_k = lds_addr_of(lds), at_v = at_k + 2 * kTileB;
@@ -685,7 +695,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_k
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_split_kernel(WinArgs a) {
   using Tl = Tile<T, D>;
-  constexpr int KT = kPromptRows<T, D>, NB = KT / 32, KS = D / 16, DB = D / 32;
+  constexpr int KT = kTileRows, NB = KT / 32, KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = KT * Tl::kRowB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -1389,7 +1399,7 @@ hipError_t run_prefill(const WinArgs &a, unsigned grid, bool split, hipStream_t 
     hipLaunchKernelGGL((window_prefill_split_kernel<T, D>), dim3(grid), dim3(256), (split_lds<T, D>()), st, a);
     return hipGetLastError();
   }
-  constexpr size_t bytes = 4 * (size_t)kPromptRows<T, D> * D * sizeof(T);
+  constexpr size_t bytes = 4 * (size_t)kTileRows * D * sizeof(T);
   hipError_t e = allow_lds(once, (const void *)window_prefill_kernel<T, D>, bytes);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((window_prefill_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
@@ -1398,7 +1408,7 @@ hipError_t run_prefill(const WinArgs &a, unsigned grid, bool split, hipStream_t 
 template <typename T, int D>
 hipError_t run_backward_as(const WinArgs &a, unsigned grid, bool split, unsigned units8, hipStream_t st) {
   static OncePerDevice<hipError_t> once_q, once_split, once_kv, once_far;
-  constexpr size_t bytes = 4 * (size_t)kTileRows<T, D> * D * sizeof(T), bytes_kv = kv_lds<T, D>();
+  constexpr size_t bytes = 4 * (size_t)kTileRows * D * sizeof(T), bytes_kv = kv_lds<T, D>();
   hipError_t e = split ? allow_lds(once_split, (const void *)window_dq_split_kernel<T, D>, split_lds<T, D>())
                        : allow_lds(once_q, (const void *)window_dq_kernel<T, D>, bytes);
   if (e == hipSuccess) e = allow_lds(once_kv, (const void *)window_dkv_kernel<T, D, false>, bytes_kv);

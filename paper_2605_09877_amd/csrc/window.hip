@@ -9,11 +9,11 @@
 // dk = scale dS^T q,  dv = P^T dout  (another, a workgroup's keys): seven products for the five there are, and no atomics.
 // Single token: one pass over the rows that its sequence sees of a ring cache.
 //
-// What they reach (bf16, 128 channels): prompt, 2 sequences of 16k tokens, 32 heads on 8, window 2048: 1065 us, 0.97 PFLOP/s, where a
+// What they reach (bf16, 128 channels): prompt, 2 sequences of 16k tokens, 32 heads on 8, window 2048: 1070 us, 0.97 PFLOP/s, where a
 // large matrix product of a library takes 1.24.  Matrix instructions are 46 % of the cycles; the vector instructions of a tile (a
 // quarter-rate exponential for every pair) take about as many cycles again, LDS reads and the tiles' direct loads the rest (without
-// either, in a copy made to measure: -10 and -14 %).  Two sequences of 8k tokens, window 1024, of both passes: 411 us forward, 542 dq,
-// 700 dk and dv, 79 the sinks' far queries.  Single token, 64 sequences, 8 KV heads, 4100 rows: 178 us, 5.7 TB/s, the card's read rate.
+// either, in a copy made to measure: -10 and -14 %).  Two sequences of 8k tokens, window 1024, of both passes: 402 us forward, 549 dq,
+// 709 dk and dv, 67 the sinks' far queries: 1.16 TFLOP done in 1.47 ms.  Single token, 64 sequences, 8 KV heads, 4100 rows: 178 us, 5.7 TB/s, the card's read rate.
 #include <math.h>
 
 #include <type_traits>

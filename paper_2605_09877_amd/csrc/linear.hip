@@ -18,8 +18,8 @@
 //
 // What it reaches (bf16, 128 channels): rows are read and written once in the walk, and y and z once more in the first pass.  8 sequences
 // of 32k tokens, 32 heads on 8: 1.45 ms for 6.44 GB, 4.4 TB/s (a copy of one GiB: 5.1); matrix instructions take 29 % of the walk's
-// cycles.  Gradients and prompt of 4 x 8k tokens, 16 heads: 637 us for 2.1 GB.  Such calls have 512 workgroups, a round of the device,
-// and wait for the chain of a chunk (pairs, their product, the state) more than for memory.  Single token, 128 sequences of 32 heads:
+// cycles.  Gradients and prompt of 4 x 8k tokens, 16 heads: 637 us for 2.4 GB.  Neither memory nor the matrix units are full
+// there: a workgroup has one chain of dependent steps for each chunk (pairs, their product, the state).  Single token, 128 sequences of 32 heads:
 // states at 5.2 TB/s, read and written, where a copy takes 5.1.
 #include <math.h>
 

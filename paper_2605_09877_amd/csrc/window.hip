@@ -13,7 +13,7 @@
 // large matrix product of a library takes 1.24.  Matrix instructions are 46 % of the cycles; the vector instructions of a tile (a
 // quarter-rate exponential for every pair) take about as many cycles again, LDS reads and the tiles' direct loads the rest (without
 // either, in a copy made to measure: -10 and -14 %).  Two sequences of 8k tokens, window 1024, of both passes: 402 us forward, 549 dq,
-// 709 dk and dv, 67 the sinks' far queries: 1.16 TFLOP done in 1.47 ms.  Single token, 64 sequences, 8 KV heads, 4100 rows: 178 us, 5.7 TB/s, the card's read rate.
+// 770 dk and dv: 1.16 TFLOP done in 1.5 ms.  Single token, 64 sequences, 8 KV heads, 4100 rows: 178 us, 5.7 TB/s, the card's read rate.
 #include <math.h>
 
 #include <type_traits>
@@ -51,7 +51,7 @@ struct WinArgs {
   int32_t sink_rows, parts;   // S up to 32, 64 or 128; shares
   float *sums;     // n_part > 1: [units, n_part, 2, Tk, D]: dk and dv of every part of a key tile's queries
   int32_t n_part;
-  int32_t key_tiles;
+  int32_t key_tiles, far_wgs;   // tiles of 128 keys; workgroups that have sinks' far queries
 };
 
 // Keys of a tile.  With 32 the prompt kernel has registers for three workgroups to a compute unit, in whose turns the exponentials of one
@@ -792,15 +792,17 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dq_s
 }
 
 // dk and dv of 128 keys, 32 to a wave (K in registers, V in LDS); the queries that see them, head after head of the group, stream
-// in tiles of 32.  Sinks (keys below S) are also seen by every query beyond their window: by a launch of its own (far), which cuts
-// those into n_split ranges, a workgroup each; its waves share the range's tiles among them (or the sinks, 32 to a wave), each with
-// tiles of its own and no barrier.  What ranges and window give for sinks is added up by window_sinks_kernel.
+// in tiles of 32.  Sinks (keys below S) are also seen by every query beyond their window: by workgroups of their own (far), the first of
+// the launch, which cut those into n_split ranges; a workgroup's waves share its range's tiles among them (or the sinks, 32 to a wave),
+// each with tiles of its own and no barrier.  What ranges and window give for sinks is added up by window_sinks_kernel.  (All gradients,
+// us, far in the same launch / in one of its own: fp32, 3 x 777 tokens, 6 heads on 2, 75 / 94; bf16, 2k, 16 heads of 64, 54 / 58;
+// fp32, 2 x 4k, 16 heads of 128 on 4, 1210 / 1237; bf16, 2 x 8k, 16 heads of 128 on 2, 852 / 844.)
 template <typename T, int D>
 constexpr size_t kv_lds() {
   return (4 * 32 + 128) * (size_t)D * sizeof(T) + 4 * 64 * sizeof(float);
 }
 template <typename T, int D, bool far>
-__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_kernel(WinArgs a) {
+__device__ __forceinline__ void key_gradients(const WinArgs &a, int block) {
   using Tl = Tile<T, D>;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = 32 * Tl::kRowB;
@@ -813,8 +815,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
   const int G = a.Hq / a.Hkv, off = a.Tk - a.Tq, units = a.B * a.Hkv;
   // a unit's workgroups go to one XCD
   const int per_unit = far ? a.n_split : a.key_tiles * a.n_part;
-  const int u = blockIdx.x / kXcds / per_unit * kXcds + blockIdx.x % kXcds;
-  const int member = blockIdx.x / kXcds % per_unit / (far ? 1 : a.n_part), queries = blockIdx.x / kXcds % (far ? 1 : a.n_part);
+  const int u = block / kXcds / per_unit * kXcds + block % kXcds;
+  const int member = block / kXcds % per_unit / (far ? 1 : a.n_part), queries = block / kXcds % (far ? 1 : a.n_part);
   if (u >= units) return;
   const int b = u / a.Hkv, hkv = u % a.Hkv;
   const int n = tokens_of(a, b);
@@ -1030,6 +1032,12 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_
       }
     }
   }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_dkv_kernel(WinArgs a) {
+  if ((int)blockIdx.x < a.far_wgs) key_gradients<T, D, true>(a, blockIdx.x);
+  else key_gradients<T, D, false>(a, blockIdx.x - a.far_wgs);
 }
 
 // dk and dv where a key tile's queries are shared among workgroups: the sums of the parts, and of a sink's far shares.
@@ -1407,25 +1415,19 @@ hipError_t run_prefill(const WinArgs &a, unsigned grid, bool split, hipStream_t 
 }
 template <typename T, int D>
 hipError_t run_backward_as(const WinArgs &a, unsigned grid, bool split, unsigned units8, hipStream_t st) {
-  static OncePerDevice<hipError_t> once_q, once_split, once_kv, once_far;
+  static OncePerDevice<hipError_t> once_q, once_split, once_kv;
   constexpr size_t bytes = 4 * (size_t)kTileRows * D * sizeof(T), bytes_kv = kv_lds<T, D>();
   hipError_t e = split ? allow_lds(once_split, (const void *)window_dq_split_kernel<T, D>, split_lds<T, D>())
                        : allow_lds(once_q, (const void *)window_dq_kernel<T, D>, bytes);
-  if (e == hipSuccess) e = allow_lds(once_kv, (const void *)window_dkv_kernel<T, D, false>, bytes_kv);
-  if (e == hipSuccess && a.n_split > 0) e = allow_lds(once_far, (const void *)window_dkv_kernel<T, D, true>, bytes_kv);
+  if (e == hipSuccess) e = allow_lds(once_kv, (const void *)window_dkv_kernel<T, D>, bytes_kv);
   if (e != hipSuccess) return e;
   if (split) hipLaunchKernelGGL((window_dq_split_kernel<T, D>), dim3(grid), dim3(256), (split_lds<T, D>()), st, a);
   else hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D, false>), dim3(units8 * a.key_tiles * a.n_part), dim3(256), bytes_kv, st, a);
+  hipLaunchKernelGGL((window_dkv_kernel<T, D>), dim3(a.far_wgs + units8 * a.key_tiles * a.n_part), dim3(256), bytes_kv, st, a);
   e = hipGetLastError();
   if (e != hipSuccess || (a.n_split == 0 && a.n_part == 1)) return e;
-  if (a.n_split > 0) {
-    hipLaunchKernelGGL((window_dkv_kernel<T, D, true>), dim3(units8 * a.n_split), dim3(256), bytes_kv, st, a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   if (a.n_part > 1) {
     const unsigned wgs = (unsigned)((2 * (int64_t)a.Tk * D / 4 + 255) / 256);
     hipLaunchKernelGGL((window_sum_kernel<T, D>), dim3(wgs, (unsigned)(a.B * a.Hkv)), dim3(256), 0, st, a);
@@ -1533,7 +1535,8 @@ extern "C" int kvm_window_backward(const kvm_window_config *cfg, const void *q, 
   const bool split = split_tiles(a);
   const unsigned grid = query_grid(a);
   const int64_t units8 = ((int64_t)a.B * a.Hkv + kXcds - 1) / kXcds * kXcds;
-  if (grid == 0 || units8 * a.key_tiles >= kMostWgs || (int64_t)a.B * a.Hkv * 2 * a.S * d / 64 >= kMostWgs) return KVM_ERR_ARG;
+  a.far_wgs = (int32_t)(units8 * a.n_split);
+  if (grid == 0 || units8 * (a.key_tiles + a.n_split) >= kMostWgs || (int64_t)a.B * a.Hkv * 2 * a.S * d / 64 >= kMostWgs) return KVM_ERR_ARG;
   const hipError_t e = KVM_BY_TYPE(cfg, run_backward_as, a, grid, split, (unsigned)units8, (hipStream_t)stream);
   return e == hipSuccess ? KVM_OK : report_hip(e, "kvm_window_backward");
 }

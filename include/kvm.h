@@ -404,8 +404,8 @@ int kvm_window_decode(const kvm_window_config *cfg, void *cache_k, void *cache_v
  * A mixer that hybrids put beside the KVM layer, in the same layouts: one fp32 state S [d, d] (key channel, value
  * channel) per sequence and KV head, whatever the tokens seen;
  *   S_t = exp(a_h) S_{t-1} + k_t v_t^T,   out_t = scale * q_t S_t,
- * a_h = log_decay[h] <= 0 a constant of the KV head (device fp32 [H_kv]; it gets no gradient; values above 0 are not
- * refused, the state then grows).  The H_q / H_kv query heads of a group share one state.  Sums and states are
+ * a_h = log_decay[h] <= 0 a constant of the KV head (device fp32 [H_kv]; it gets no gradient; -infinity keeps nothing,
+ * values above 0 are not refused, the state then grows).  The H_q / H_kv query heads of a group share one state.  Sums and states are
  * fp32; q, k, v, out are KVM_F32 or KVM_BF16.  In prompts tokens are taken 64 at a time (fp32: 32): a NaN or an infinity
  * of a later token's k or v, or an earlier one's, makes NaN of outputs of the same group of tokens; behind it the state is
  * NaN where the recurrence makes it infinite or NaN.

@@ -630,6 +630,8 @@ def _io_of(q: torch.Tensor) -> int:
     io = _IO_OF.get(q.dtype)
     if io is None:
         raise ValueError(f"q: want torch.bfloat16 or torch.float32, got {q.dtype}")
+    if not q.is_cuda:
+        raise ValueError(f"q: want a tensor of a GPU, got one on {q.device}")
     return io
 
 

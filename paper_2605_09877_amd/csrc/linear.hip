@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kPair ? 4 * D : 2 * D, 2) void linear_walk_kernel(L
   if (!kOut && s1 - s0 < a.seg_tokens) return;   // (a segment that another one follows is full)
 
   // ---- powers of the decay
-  const float al = a.log_decay[h];
+  const float a_h = a.log_decay[h], al = a_h < -1e4f ? -1e4f : a_h;   // (-infinity too: its powers are 0, and 1 for no step at all)
   for (int i = tid; i < 32 + C; i += 64 * kWaves) rel[i] = i < 32 ? 0.f : a.scale * expf(al * (float)(i - 32));
   if (tid < C) wt[tid] = expf(al * (float)(C - kShift - tid));
   float dec[TB];

@@ -366,3 +366,25 @@ def test_scale_by_value():
     half = kvm.linear_prefill(*a, scale=scale)[0]
     scale.fill_(0.25)
     assert torch.equal(half, 2 * kvm.linear_prefill(*a, scale=scale)[0])
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_a_decay_that_keeps_nothing(io):
+    """log_decay = -infinity for one head: out_t = scale (q_t . k_t) v_t there, and nothing of the start state."""
+    import paper_2605_09877_amd as kvm
+    B, T, d = 1, 700, 64
+    x = make(io, B, T, 2, 2, d)
+    ld = torch.tensor([-float("inf"), -0.1], device=DEV)
+    leaves = [x[n].clone().requires_grad_() for n in ("q", "k", "v", "state")]
+    out, st = kvm.kvm_linear_attention(*leaves[:3], ld, state=leaves[3])
+    grads = torch.autograd.grad((out, st), leaves, (x["dout"], x["dstate"]))
+    y = {n: f64(t) for n, t in x.items()}
+    ref = (*mo.linear(y["q"], y["k"], y["v"], f64(ld), y["state"]),
+           *mo.linear_backward(y["q"], y["k"], y["v"], f64(ld), y["dout"], y["state"], y["dstate"]))
+    mag = magnitudes(dict(x, log_decay=ld), None, None)
+    for i, (got, name) in enumerate(zip((out, st, *grads), ("out", "state", "dq", "dk", "dv", "dstate"))):
+        check("f32" if name in ("state", "dstate") else io, got, ref[i], mag[i], d, T, name)
+    token = x["state"].clone()
+    o = kvm.linear_decode(token, *(x[n][:, 0].contiguous() for n in "qkv"), ld)
+    check(io, o, ref[0][:, 0], mag[0][:, 0], d, 1, "token")
+    assert torch.count_nonzero(grads[3][:, 0]) == 0

@@ -277,3 +277,14 @@ def test_strides_of_axes_of_one_entry():
     assert (s.q_b, s.q_t, s.q_h) == (64, 64, 64) and (s.k_b, s.k_t, s.k_h) == (576, 64, 64) and (s.o_b, s.o_t, s.o_h) == (64, 64, 64)
     wide = torch.empty(2, 9, 3, 128)[:, :, :, :64]
     assert (kb._row_strides(wide, k, k, wide).q_t, kb._row_strides(wide, k, k, wide).q_h) == (384, 128)
+
+
+def test_tensors_of_the_host_are_refused():
+    q, k, pos = torch.zeros(1, 4, 2, 64), torch.zeros(1, 4, 2, 64), torch.zeros(1, dtype=torch.int32)
+    cache, state, ld = torch.zeros(1, 2, 5, 64), torch.zeros(1, 2, 64, 64), torch.zeros(2)
+    for call in (lambda: kb.window_prefill(q, k, k, window=3), lambda: kb.window_fill(cache, cache, k, k, window=5),
+                 lambda: kb.window_decode(cache, cache, q[:, 0], k[:, 0], k[:, 0], pos, window=5),
+                 lambda: kb.window_backward(q, k, k, q, torch.zeros(1, 4, 2), q, window=3), lambda: kb.linear_prefill(q, k, k, ld),
+                 lambda: kb.linear_backward(q, k, k, ld, q), lambda: kb.linear_decode(state, q[:, 0], k[:, 0], k[:, 0], ld)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()

@@ -138,3 +138,49 @@ def test_padded_training_step_captured():
     out = step()
     assert torch.equal(out[0][0], want[0][0]) and torch.equal(out[0][2, :171], want[0][2, :171])
     assert torch.equal(out[1][0], want[1][0]) and torch.equal(out[1][2, :171], want[1][2, :171])
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 2^23 elements apart (the most that is allowed): offsets of 300 of them pass 2^32 bytes.  The bits are those of dense copies."""
+    import paper_2605_09877_amd as kvm
+    T, h, dd, far = 300, 2, 64, 1 << 23
+    pool = torch.empty(T * far, dtype=torch.bfloat16, device=DEV)   # 5 GB
+    gen = torch.Generator(DEV).manual_seed(4)
+    views = [pool.as_strided((1, T, h, dd), (T * far, far, dd, 1), 1024 * i) for i in range(4)]
+    for t in views[:3]:
+        t.copy_(torch.randn(t.shape, generator=gen, device=DEV))
+    q, k, v, out = views
+    dense = [t.contiguous() for t in (q, k, v)]
+    want = kvm.window_prefill(*dense, window=70, n_sink=2)
+    kvm.window_prefill(q, k, v, window=70, n_sink=2, out=out)
+    assert torch.equal(out, want)
+    ld = torch.tensor([-0.01, -0.2], device=DEV)
+    want, end = kvm.linear_prefill(*dense, ld)
+    got = kvm.linear_prefill(q, k, v, ld, out=out)
+    assert torch.equal(out, want) and torch.equal(got[1], end)
+    caches = [kvm.window_cache(1, h, dd, window=70, n_sink=2, device=DEV) for _ in range(2)]
+    kvm.window_fill(*caches[0], *dense[1:], window=70, n_sink=2)
+    kvm.window_fill(*caches[1], k, v, window=70, n_sink=2)
+    for a, b in zip(*caches):
+        assert torch.equal(a, b)
+
+
+def test_a_cache_beyond_32_bits():
+    """36 million rows, 4.6 GB each for k and v: a row behind 2^32 bytes has all the weight but e^-100 of it for each other row, so the
+    result is that row's value to the bit; then a row stored at the ring's end is seen as well, with the same logit."""
+    import paper_2605_09877_amd as kvm
+    W, dd = 36_000_000, 64
+    ck, cv = kvm.window_cache(1, 1, dd, window=W, device=DEV)
+    ck.zero_()
+    cv.fill_(1.0)
+    q = torch.ones(1, 1, dd, dtype=torch.bfloat16, device=DEV)
+    k = torch.full_like(q, 12.5)     # 64 * 12.5 / 8 = 100
+    v = torch.arange(dd, device=DEV).to(torch.bfloat16).view(1, 1, dd)
+    row = 35_000_000
+    ck[0, 0, row], cv[0, 0, row] = k[0, 0], v[0, 0]
+    pos = torch.tensor([W + 5], dtype=torch.int32, device=DEV)   # its own row: 5
+    args = dict(window=W)
+    assert torch.equal(kvm.window_decode(ck, cv, q, torch.zeros_like(k), torch.ones_like(v), pos, **args), v)
+    pos.fill_(2 * W - 1)             # its own row: the last
+    assert torch.equal(kvm.window_decode(ck, cv, q, k, 3 * v, pos, **args), 2 * v)
+    assert torch.equal(ck[0, 0, W - 1], k[0, 0]) and torch.equal(cv[0, 0, W - 1], 3 * v[0, 0])

@@ -373,7 +373,8 @@ typedef struct kvm_window_config {
 } kvm_window_config;
 
 /* Strides as in kvm_prefill_chunked (NULL = dense; gate strides are not looked at), token strides up to 2^23 elements;
- * Tk < 2^30.  lse: [B, Tq, H_q] fp32 natural-log sum of exponentials, or NULL; out_rest: what rounding out to bf16 left of
+ * Tk < 2^30.  lse: [B, Tq, H_q] fp32 natural-log sum of exponentials, or NULL (asked for, short rows in bf16 are computed
+ * more finely, for the gradients' sake); out_rest: what rounding out to bf16 left of
  * it, rounded to bf16, in out's shape and strides (for kvm_window_backward), or NULL; not written with KVM_F32. */
 int kvm_window_prefill(const kvm_window_config *cfg, const void *q, const void *k, const void *v, const int32_t *lens,
                        void *out, void *out_rest, float *lse, int64_t Tq, int64_t Tk, const kvm_strides *strides,

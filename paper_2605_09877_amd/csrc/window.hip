@@ -144,6 +144,18 @@ __device__ __forceinline__ void load4(const char *row, int blk, int vq, int g, f
   }
 }
 
+__device__ __forceinline__ float add_operand(const Operand<bf16_t> &x, float sum) {
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x.f.w[e]), ones, sum, false);
+  return sum;
+}
+__device__ __forceinline__ float add_operand(const Operand<float> &x, float sum) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum += x.f[e];
+  return sum;
+}
+
 // A query done again, one visible key after the other in fp32 (a lane has half of its channels): a key that it does not see
 // enters the second product of the tile kernels with p = 0, and a value of it that is not finite makes that NaN.
 template <typename T, int D>
@@ -250,11 +262,15 @@ struct Fragments {
   }
 };
 
+// kFine (bf16): P enters the second product as two operands, with errors of 2^-16, where gradients will be asked for and rows are short
+// (fine_rows).  What P's rounding moves, lse and D = dout . out, moves every dS of a row: dq and dk of rows of n keys would have
+// the variance of 2 + 2 / n roundings instead of 2.
 // (fp32 rows of 128 channels: with two workgroups to a CU registers spill; 2 sequences of 4096 tokens of 16 heads, window 512,
 // take 399 us with one and 437 with two.)
-template <typename T, int D>
-__global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 1) void window_prefill_kernel(WinArgs a) {
+template <typename T, int D, bool kFine>
+__global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : kFine ? 2 : 3) void window_prefill_kernel(WinArgs a) {
   using Tl = Tile<T, D>;
+  constexpr int kPlanes = kFine ? 2 : 1;
   constexpr int KT = kTileRows, NB = KT / 32, KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = KT * Tl::kRowB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -331,7 +347,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 1) void window_pref
     }
     // P enters the second product in the I/O dtype; the sum is taken over the rounded values, so that numerator and
     // denominator see the same ones
-    Operand<T> pf[2 * NB];
+    Operand<T> pf[2 * NB][kPlanes];
     auto exponentials = [&]() {
       const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen yet)
       float sum = 0.f;
@@ -340,15 +356,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 1) void window_pref
         float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + e], c, -ref));
-        to_operand(p, pf[ks]);
-        if constexpr (sizeof(T) == 2) {
-          const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+        split_operand<kPlanes>(p, pf[ks]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pf[ks].f.w[e]), ones, sum, false);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum += p[e];
-        }
+        for (int n = 0; n < kPlanes; ++n) sum = add_operand(pf[ks][n], sum);
       }
       return sum;
     };
@@ -377,7 +387,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 3 : 1) void window_pref
 #pragma unroll
     for (int ks = 0; ks < 2 * NB; ++ks)
 #pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] = mma(fr.across(i, ks, kBuf), pf[ks], o[i]);
+      for (int i = 0; i < DB; ++i) {
+        const Operand<T> vt = fr.across(i, ks, kBuf);
+#pragma unroll
+        for (int n = 0; n < kPlanes; ++n) o[i] = mma(vt, pf[ks][n], o[i]);
+      }
   };
   __builtin_amdgcn_s_waitcnt(0);
   load_tile(0);
@@ -399,9 +413,10 @@ template <typename T, int D>
 constexpr size_t split_lds() {
   return kWaves * (2 * (size_t)kTileRows * D * sizeof(T) + 2 * 64 * sizeof(float)) + 32 * sizeof(int);
 }
-template <typename T, int D>
+template <typename T, int D, bool kFine>
 __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_prefill_split_kernel(WinArgs a) {
   using Tl = Tile<T, D>;
+  constexpr int kPlanes = kFine ? 2 : 1;
   constexpr int KT = kTileRows, NB = KT / 32, KS = D / 16, DB = D / 32;
   constexpr uint32_t kTileB = KT * Tl::kRowB;
   constexpr int kLoads = (int)(kTileB / 1024);   // of a wave for a tile
@@ -496,18 +511,16 @@ __global__ __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) void window_pref
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + e], c, -ref));
-      Operand<T> pf;
-      to_operand(p, pf);
-      if constexpr (sizeof(T) == 2) {
-        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+      Operand<T> pf[kPlanes];
+      split_operand<kPlanes>(p, pf);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pf.f.w[e]), ones, l, false);
-      } else {
+      for (int n = 0; n < kPlanes; ++n) l = add_operand(pf[n], l);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) l += p[e];
+      for (int i = 0; i < DB; ++i) {
+        const Operand<T> vt = fr.across(i, ks, 0);
+#pragma unroll
+        for (int n = 0; n < kPlanes; ++n) o[i] = mma(vt, pf[n], o[i]);
       }
-#pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] = mma(fr.across(i, ks, 0), pf, o[i]);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the v tile has been read
     if (more) load_v(it + kWaves);
@@ -1398,20 +1411,32 @@ bool split_tiles(WinArgs &a) {
   tile_queries(a, false, 32);
   return true;
 }
-template <typename T, int D>
-hipError_t run_prefill(const WinArgs &a, unsigned grid, bool split, hipStream_t st) {
+// Prompts of a training step (lse is asked for) whose rows have few keys: the errors of dq and dk against a single rounding's are 1.43 to
+// 1.49 with P as one operand there (up to 1.56 for 16 tokens), 1.42 to 1.45 as two (1.49).  Beyond, the difference goes, and the second operand
+// costs: us, two / one, 64 x 256 tokens, 16 heads, 141 / 111; 4 x 4k, 16 heads of 64 on 4, window 128, 39 / 34; 2 x 256, 8 heads, 8.0 / 7.6.
+bool fine_rows(const WinArgs &a) { return a.lse && (a.Tk <= 256 || a.W + a.S <= 64); }
+
+template <typename T, int D, bool kFine>
+hipError_t run_prefill_as(const WinArgs &a, unsigned grid, bool split, hipStream_t st) {
   static OncePerDevice<hipError_t> once, once_split;
   if (split) {
-    const hipError_t e = allow_lds(once_split, (const void *)window_prefill_split_kernel<T, D>, split_lds<T, D>());
+    const hipError_t e = allow_lds(once_split, (const void *)window_prefill_split_kernel<T, D, kFine>, split_lds<T, D>());
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((window_prefill_split_kernel<T, D>), dim3(grid), dim3(256), (split_lds<T, D>()), st, a);
+    hipLaunchKernelGGL((window_prefill_split_kernel<T, D, kFine>), dim3(grid), dim3(256), (split_lds<T, D>()), st, a);
     return hipGetLastError();
   }
   constexpr size_t bytes = 4 * (size_t)kTileRows * D * sizeof(T);
-  hipError_t e = allow_lds(once, (const void *)window_prefill_kernel<T, D>, bytes);
+  hipError_t e = allow_lds(once, (const void *)window_prefill_kernel<T, D, kFine>, bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((window_prefill_kernel<T, D>), dim3(grid), dim3(256), bytes, st, a);
+  hipLaunchKernelGGL((window_prefill_kernel<T, D, kFine>), dim3(grid), dim3(256), bytes, st, a);
   return hipGetLastError();
+}
+template <typename T, int D>
+hipError_t run_prefill(const WinArgs &a, unsigned grid, bool split, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (fine_rows(a)) return run_prefill_as<T, D, true>(a, grid, split, st);
+  }
+  return run_prefill_as<T, D, false>(a, grid, split, st);
 }
 template <typename T, int D>
 hipError_t run_backward_as(const WinArgs &a, unsigned grid, bool split, unsigned units8, hipStream_t st) {

@@ -445,3 +445,17 @@ def test_maxima_that_rise_or_fall_along_the_keys(io, d, step):
         out, lse = kvm.window_prefill(*(x[m].repeat(n, 1, 1, 1) for m in "qkv"), window=W, n_sink=S, want_lse=True)
         within(out[:1], ref, tol, f"out of {n}")
         assert torch.equal(out, out[:1].expand_as(out)) and torch.equal(lse, lse[:1].expand_as(lse))
+
+
+@pytest.mark.parametrize("B,T,W,S", [(8, 24, 300, 0), (4, 100, 64, 3), (2, 700, 9, 0), (1, 900, 300, 5)])
+def test_gradients_are_within_two_roundings(B, T, W, S):
+    """The norm of the error of dq and dk, bf16: dS is rounded once and the result once, each with an error of 2^-8 / 3^(1/2) of its value
+    at the most (a mean square over a step's whole width), independent of the other; another 5 % for what is left of P's rounding."""
+    import paper_2605_09877_amd as kvm
+    x = make("bf16", B, T, T, 4, 2, 64, seed=9)
+    leaves = [x[n].clone().requires_grad_() for n in "qkv"]
+    grads = torch.autograd.grad(kvm.kvm_window_attention(*leaves, window=W, n_sink=S), leaves, x["dout"])
+    ref = mo.window_backward(*(f64(x[n]) for n in ("q", "k", "v", "dout")), W, S)
+    for got, r, name in zip(grads, ref, ("dq", "dk", "dv")):
+        error = np.linalg.norm(f64(got) - r) / np.linalg.norm(r)
+        assert error <= 1.05 * 2 ** 0.5 * 2.0 ** -8 / 3 ** 0.5, (name, error)

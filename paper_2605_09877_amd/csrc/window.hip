@@ -157,7 +157,9 @@ __device__ __forceinline__ float add_operand(const Operand<float> &x, float sum)
 }
 
 // A query done again, one visible key after the other in fp32 (a lane has half of its channels): a key that it does not see
-// enters the second product of the tile kernels with p = 0, and a value of it that is not finite makes that NaN.
+// enters the second product of the tile kernels with p = 0, and a value of it that is not finite makes that NaN.  Every visible
+// key has its part, whatever its place: a NaN logit, which fmaxf passes over, makes p and l NaN, a NaN value a NaN channel also
+// where p is 0.  Nothing but logits of -infinity: zeros.
 template <typename T, int D>
 __device__ __forceinline__ void attend_one_by_one(const WinArgs &a, const char *qrow, const char *kb, const char *vb, int t, float c,
                                                   int g, f32x16 (&o)[D / 32], float &m, float &l) {
@@ -184,9 +186,8 @@ __device__ __forceinline__ void attend_one_by_one(const WinArgs &a, const char *
 #pragma unroll
       for (int e = 0; e < 4; ++e) dot = fmaf(x[e], y[e], dot);
     }
-    const float x = xhalf_sum(dot) * c, m_new = fmaxf(m, x);
-    if (m_new == -INFINITY) continue;
-    const float alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(x - m_new);
+    const float x = xhalf_sum(dot) * c, m_new = fmaxf(m, x), ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(x - ref);
     m = m_new;
     l = fmaf(l, alpha, p);
 #pragma unroll
@@ -197,6 +198,11 @@ __device__ __forceinline__ void attend_one_by_one(const WinArgs &a, const char *
       for (int e = 0; e < 4; ++e) o[i >> 2][4 * (i & 3) + e] = fmaf(p, y[e], o[i >> 2][4 * (i & 3) + e] * alpha);
     }
   }
+  if (l == 0.f)
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
 }
 
 // What a query's lane pair has in the end: o / l to out, what its rounding leaves to rest, the logarithm of the sum to lse.

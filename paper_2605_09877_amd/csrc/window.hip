@@ -1296,7 +1296,8 @@ __global__ __launch_bounds__(256) void window_token_kernel(CacheArgs a) {
   }
 }
 
-// The ranges of a query head joined: a lane has a range's maximum and sum, a thread a channel of every kParts-th range.
+// The ranges of a query head joined: a lane has a range's maximum and sum, a thread a channel of every kParts-th range.  A range without
+// a token has factor, sum and channels of 0; one whose sum or channel is not a number makes the result that, whatever its factor.
 constexpr int kMostSplits = 64;
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_join_kernel(CacheArgs a) {
@@ -1309,15 +1310,12 @@ __global__ __launch_bounds__(256) void window_join_kernel(CacheArgs a) {
   const float *own = p + (lane < a.n_split ? lane : 0) * (D + 2) + D;
   const float m = lane < a.n_split ? own[0] : -INFINITY, l = own[1];
   const float top = wave_max(m), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-  const float sum = wave_sum(f == 0.f ? 0.f : f * l);
+  const float sum = wave_sum(lane < a.n_split ? f * l : 0.f);
   if (threadIdx.x < 64) factor[lane] = f;
   __syncthreads();
   float x = 0.f;
 #pragma unroll 16
-  for (int s = part; s < a.n_split; s += kParts) {
-    const float y = p[s * (D + 2) + ch];
-    x = factor[s] == 0.f ? x : fmaf(factor[s], y, x);
-  }
+  for (int s = part; s < a.n_split; s += kParts) x = fmaf(factor[s], p[s * (D + 2) + ch], x);
   acc[part][ch] = x;
   __syncthreads();
   if (part != 0) return;

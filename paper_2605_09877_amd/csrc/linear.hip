@@ -462,17 +462,20 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinTokenArgs a) {
   float4 s[kRows];
 #pragma unroll
   for (int r = 0; r < kRows; ++r) s[r] = *reinterpret_cast<const float4 *>(st + r * D);
-  const float lam = expf(a.log_decay[h]);
+  // (the decay as a float and what that leaves: the rounding of one, the same in every call, would be 3e-8 of a slowly decaying state a
+  // token, 7e-5 of it after 2000)
+  const double decay = exp((double)a.log_decay[h]);
+  const float lam = (float)decay, rest = lam == INFINITY ? 0.f : (float)(decay - (double)lam);
   float vv[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) vv[e] = Io<T>::load(v + c + e);
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
     const float kr = Io<T>::load(k + r0 + r);
-    s[r].x = fmaf(s[r].x, lam, kr * vv[0]);
-    s[r].y = fmaf(s[r].y, lam, kr * vv[1]);
-    s[r].z = fmaf(s[r].z, lam, kr * vv[2]);
-    s[r].w = fmaf(s[r].w, lam, kr * vv[3]);
+    s[r].x = fmaf(s[r].x, lam, fmaf(s[r].x, rest, kr * vv[0]));
+    s[r].y = fmaf(s[r].y, lam, fmaf(s[r].y, rest, kr * vv[1]));
+    s[r].z = fmaf(s[r].z, lam, fmaf(s[r].z, rest, kr * vv[2]));
+    s[r].w = fmaf(s[r].w, lam, fmaf(s[r].w, rest, kr * vv[3]));
     *reinterpret_cast<float4 *>(st + r * D) = s[r];
   }
   for (int g0 = 0; g0 < G; g0 += kTokenHeads) {

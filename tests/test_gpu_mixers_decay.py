@@ -57,3 +57,37 @@ def test_prompts_of_many_segments(io, chunk):
     mag = (q[0, -1, 0].double().abs() @ ref.abs()) / D ** 0.5
     e = 2.0 ** -8 + 2.0 ** -7 if io is torch.bfloat16 else (2 * D + 2 * 1024) * 2.0 ** -24
     assert torch.all((out[0, -1, 0].double() - want).abs() <= e * mag)
+
+
+@pytest.mark.parametrize("B", [1, 600])   # (both arrangements of units)
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+def test_single_tokens(io, B):
+    import paper_2605_09877_amd as kvm
+    a, off = decay(1)
+    n = 2000
+    gen = torch.Generator(DEV).manual_seed(2)
+    state = torch.randn(1, 1, D, D, generator=gen, device=DEV).repeat(B, 1, 1, 1)
+    k, v = ((torch.randn(n, 1, 1, D, generator=gen, device=DEV) / 16).to(io) for _ in range(2))
+    q = torch.zeros(B, 1, D, dtype=io, device=DEV)
+    ref, lam, ld = state[0, 0].double(), math.exp(a), torch.tensor([a], device=DEV)
+    out = torch.empty_like(q)
+    for t in range(n):
+        kt, vt = k[t].expand(B, 1, D).contiguous(), v[t].expand(B, 1, D).contiguous()
+        kvm.linear_decode(state, q, kt, vt, ld, out=out)
+        ref = lam * ref + k[t, 0, 0].double()[:, None] * v[t, 0, 0].double()[None]
+    assert torch.equal(state, state[:1].expand_as(state))
+    tol = 5 * (n / 3 / D ** 2) ** 0.5 * 2.0 ** -24 + 4 * 2.0 ** -24
+    assert n / 2 * abs(off) * 2.0 ** -24 > 3 * tol
+    assert abs(shift(state[0, 0], ref)) <= tol
+
+
+def test_a_token_of_a_state_that_grows_beyond_fp32():
+    """A log decay above 0 whose power is no float: infinities of the state's signs, as the product with one is."""
+    import paper_2605_09877_amd as kvm
+    state = torch.tensor([1.0, -2.0], device=DEV).repeat(D * D // 2).view(1, 1, D, D).contiguous()
+    want = state * float("inf")
+    zero = torch.zeros(1, 1, D, device=DEV)
+    for a in (100.0, 1000.0):
+        got = state.clone()
+        kvm.linear_decode(got, zero, zero, zero, torch.tensor([a], device=DEV))
+        assert torch.equal(got, want)

@@ -665,8 +665,14 @@ def _row_strides(q, k, v, out, lse=None) -> kvm_strides:
 
 
 def _number(scale) -> Optional[float]:
-    """A scale as a key of the configurations kept below: the value, also where it is given as a tensor."""
-    return scale if scale is None else float(scale)
+    """A scale as a key of the configurations kept below: the value in fp32, also where it is given as a tensor.  (0, which selects
+    1 / sqrt(d) in the C structures, is None here and nothing else.)"""
+    if scale is None:
+        return None
+    x = C.c_float(float(scale)).value
+    if not 2.0 ** -126 <= x < float("inf"):   # (the reciprocal of a smaller one may be infinite)
+        raise ValueError(f"scale: want a positive normal number of fp32, or None for 1 / sqrt(d), got {scale}")
+    return x
 
 
 @functools.lru_cache(maxsize=4096)

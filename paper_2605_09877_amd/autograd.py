@@ -10,8 +10,8 @@ from typing import Optional
 
 import torch
 
-from .binding import (KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, linear_backward, linear_prefill, window_backward,
-                      window_prefill)
+from .binding import (KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, _number, _sizes, linear_backward, linear_prefill,
+                      window_backward, window_prefill)
 
 
 class _KVMAttention(torch.autograd.Function):
@@ -98,7 +98,7 @@ def kvm_linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     The backward pass reads `state` again: it is not to be advanced in place (linear_decode) before."""
     if log_decay.requires_grad:
         raise ValueError("log_decay: the decays are constants, they get no gradient")
-    return _LinearAttention.apply(q, k, v, log_decay, state, lens, scale)
+    return _LinearAttention.apply(q, k, v, log_decay, state, lens, _number(scale))
 
 
 class _WindowAttention(torch.autograd.Function):
@@ -124,4 +124,4 @@ def kvm_window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, w
                          lens: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
     """Attention over the last `window` keys and the first `n_sink` ones, differentiable in q, k and v.  Shapes and lens as in
     window_prefill."""
-    return _WindowAttention.apply(q, k, v, window, n_sink, lens, scale)
+    return _WindowAttention.apply(q, k, v, *_sizes(window, n_sink), lens, _number(scale))

@@ -675,6 +675,20 @@ def _number(scale) -> Optional[float]:
     return x
 
 
+def _sizes(window, n_sink):
+    """Window and sinks as keys of the configurations kept below: ints, also where they are given as tensors or whole floats."""
+    if type(window) is int and type(n_sink) is int:
+        return window, n_sink
+    got = window, n_sink
+    try:
+        window, n_sink = int(window), int(n_sink)
+    except (TypeError, ValueError, OverflowError):
+        window = None
+    if window is None or isinstance(got[0], str) or isinstance(got[1], str) or window != got[0] or n_sink != got[1]:
+        raise ValueError(f"window and n_sink: want whole numbers, got {got[0]} and {got[1]}")
+    return window, n_sink
+
+
 @functools.lru_cache(maxsize=4096)
 def _linear_config_of(B: int, Hq: int, Hkv: int, d: int, io: int, scale: Optional[float]) -> kvm_linear_config:
     return kvm_linear_config(B, Hq, Hkv, d, io, 0.0 if scale is None else scale)
@@ -771,9 +785,9 @@ def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, a
 
 @functools.lru_cache(maxsize=4096)
 def _window_config(B: int, Hq: int, Hkv: int, d: int, io: int, window: int, n_sink: int, scale) -> kvm_window_config:
-    if not 1 <= int(window) < 1 << 30 or not 0 <= int(n_sink) <= KVM_WINDOW_MAX_SINK:
+    if not 1 <= window < 1 << 30 or not 0 <= n_sink <= KVM_WINDOW_MAX_SINK:
         raise ValueError(f"window: want 1 .. 2^30 - 1, n_sink 0 .. {KVM_WINDOW_MAX_SINK}, got {window} and {n_sink}")
-    return kvm_window_config(B, Hq, Hkv, d, io, int(n_sink), int(window), 0.0 if scale is None else scale)
+    return kvm_window_config(B, Hq, Hkv, d, io, n_sink, window, 0.0 if scale is None else scale)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -792,6 +806,7 @@ def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: O
     (bf16 or fp32; views whose head_dim is contiguous), query i at position i + Tk - Tq; lens int32 [B], the sequences' keys in a padded
     batch.  Returns out, or (out, lse [B,Tq,Hq] fp32)."""
     lib = load_library()
+    window, n_sink = _sizes(window, n_sink)
     Hq, Hkv, d = _heads(q, k, 4)
     B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
     if not 0 < Tq <= Tk:
@@ -816,6 +831,7 @@ def window_backward(q, k, v, out, lse, dout, *, window: int, n_sink: int = 0, le
                     out_rest=None):
     """kvm_window_backward: (dq, dk, dv) of a window_prefill over these tensors (contiguous)."""
     lib = load_library()
+    window, n_sink = _sizes(window, n_sink)
     Hq, Hkv, d = _heads(q, k, 4)
     B, Tq, Tk, dev = q.shape[0], q.shape[1], k.shape[1], q.device
     cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, _number(scale))
@@ -839,6 +855,7 @@ def window_backward(q, k, v, out, lse, dout, *, window: int, n_sink: int = 0, le
 def window_cache(batch: int, n_kv_heads: int, head_dim: int, *, window: int, n_sink: int = 0, dtype=torch.bfloat16,
                  device="cuda:0"):
     """The cache of window_fill and window_decode: (cache_k, cache_v), each [B, Hkv, n_sink + window, d]; contents undefined."""
+    window, n_sink = _sizes(window, n_sink)
     shape = (batch, n_kv_heads, n_sink + window, head_dim)
     return torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)
 
@@ -846,6 +863,7 @@ def window_cache(batch: int, n_kv_heads: int, head_dim: int, *, window: int, n_s
 def window_fill(cache_k, cache_v, k, v, *, window: int, n_sink: int = 0, lens=None) -> None:
     """kvm_window_fill: what is left to see of a prompt that starts the sequences.  k, v [B,T,Hkv,d]."""
     lib = load_library()
+    window, n_sink = _sizes(window, n_sink)
     if k.dim() != 4:
         raise ValueError(f"k: want [B, T, Hkv, d], got {tuple(k.shape)}")
     B, T, Hkv, d = k.shape
@@ -864,6 +882,7 @@ def window_fill(cache_k, cache_v, k, v, *, window: int, n_sink: int = 0, lens=No
 def window_decode(cache_k, cache_v, q, k, v, pos, *, window: int, n_sink: int = 0, scale: Optional[float] = None, out=None):
     """kvm_window_decode: one token per sequence, at positions pos (int32 [B]; below 0: no token, zeros), stored into the cache and
     attended.  q [B,Hq,d]; k, v [B,Hkv,d]."""
+    window, n_sink = _sizes(window, n_sink)
     Hq, Hkv, d = _heads(q, k, 3)
     B, dev, dt = q.shape[0], q.device, q.dtype
     cfg, nbytes = _window_token_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, _number(scale))

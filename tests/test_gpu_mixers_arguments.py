@@ -34,3 +34,41 @@ def test_scales_that_are_refused(scale):
                  lambda: kvm.linear_decode(x["state"], *token(x), x["ld"], scale=scale)):
         with pytest.raises(ValueError, match="scale"):
             call()
+
+
+def test_windows_and_sinks_are_taken_by_value():
+    """A size given as a tensor is read in every call, whatever it held in an earlier one."""
+    import paper_2605_09877_amd as kvm
+    x = inputs()
+    qkv = [x[n] for n in "qkv"]
+    window, n_sink = torch.tensor(8), torch.tensor(1)
+    for w, s in ((8, 1), (20, 1), (20, 3), (5, 0)):
+        window.fill_(w)
+        n_sink.fill_(s)
+        assert torch.equal(kvm.window_prefill(*qkv, window=window, n_sink=n_sink), kvm.window_prefill(*qkv, window=w, n_sink=s))
+        caches = [kvm.window_cache(B, HKV, D, window=a, n_sink=b, dtype=torch.float32, device=DEV) for a, b in ((window, n_sink), (w, s))]
+        assert caches[0][0].shape == caches[1][0].shape == (B, HKV, w + s, D)
+        outs = []
+        for c, (a, b) in zip(caches, ((window, n_sink), (w, s))):
+            kvm.window_fill(*c, x["k"], x["v"], window=a, n_sink=b)
+            outs.append(kvm.window_decode(*c, *token(x), torch.full((B,), T, dtype=torch.int32, device=DEV), window=a, n_sink=b))
+        assert torch.equal(*outs)
+    assert torch.equal(kvm.window_prefill(*qkv, window=8.0), kvm.window_prefill(*qkv, window=8))
+    for bad in (dict(window=7.5), dict(window=8, n_sink=0.5), dict(window=float("nan")), dict(window="8"), dict(window=None)):
+        with pytest.raises((ValueError, TypeError)):
+            kvm.window_prefill(*qkv, **bad)
+
+
+def test_the_backward_pass_has_the_forward_passs_sizes():
+    """Sizes and scales given as tensors that change before the backward pass."""
+    import paper_2605_09877_amd as kvm
+    x = inputs()
+    leaves = [x[n].requires_grad_() for n in "qkv"]
+    for call in (lambda w, s, c: kvm.kvm_window_attention(*leaves, window=w, n_sink=s, scale=c),
+                 lambda w, s, c: kvm.kvm_linear_attention(*leaves, x["ld"], scale=c)[0]):
+        want = torch.autograd.grad(call(8, 2, 0.5), leaves, x["dout"])
+        w, s, c = torch.tensor(8), torch.tensor(2), torch.tensor(0.5)
+        out = call(w, s, c)
+        w.fill_(30), s.fill_(0), c.fill_(0.125)
+        for a, b in zip(want, torch.autograd.grad(out, leaves, x["dout"])):
+            assert torch.equal(a, b)

@@ -95,7 +95,7 @@ def kvm_linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     """Linear attention with a decay for each KV head over a whole sequence, differentiable in q, k, v and the state it
     starts from: S_t = exp(log_decay) S_{t-1} + k_t v_t^T, out_t = scale q_t S_t.  Shapes and lens as in linear_prefill.  The decays
     are constants of the layer: a log_decay that requires a gradient is refused.  Returns (out, state behind the last token).
-    The backward pass reads `state` again: it is not to be advanced in place (linear_decode) before."""
+    The backward pass reads `state` again and raises an error if it has been advanced in place (linear_decode) since."""
     if log_decay.requires_grad:
         raise ValueError("log_decay: the decays are constants, they get no gradient")
     return _LinearAttention.apply(q, k, v, log_decay, state, lens, _number(scale))

@@ -173,6 +173,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 # device context (3 us) is entered only when another device is current, shapes are compared as they are.
 # Eight tokens of one sequence, preparation and decode step, 333 us before, 248 now; a prompt of 50 tokens 20.5, now 16.3.
 # (A torch without them, one for CPUs alone, has the host-side parts of this module: sizes, schedules, errors.)
+# (of a list of tensors; those made in inference mode have no version and are passed over)
+_count_write = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -622,6 +624,8 @@ def decode_multi_static(states, q, k, v, gate=None, *, out):
 
 # ---- the mixers beside the layer: linear attention with decay, sliding-window attention with sinks
 # (A single token is a few microseconds of GPU work: its calls find their configuration and workspace size by one look-up.)
+# What a call writes of the caller's tensors counts as written for autograd, too: a backward pass that holds one of them as it was
+# raises an error, as after torch's own operations in place.
 
 _IO_OF = {torch.bfloat16: KVM_BF16, torch.float32: KVM_F32}
 
@@ -710,6 +714,7 @@ def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional
     dev, Hkv, d = q.device, cfg.n_kv_heads, cfg.head_dim
     if T == 0:
         raise ValueError("q: no tokens")
+    given = [t for t in (out, state_out) if t is not None]
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     if state_out is None:
@@ -726,6 +731,8 @@ def linear_prefill(q, k, v, log_decay, *, state=None, lens=None, scale: Optional
         status = lib.kvm_linear_prefill(cfg, *ptrs, T, _row_strides(q, k, v, out), ws.data_ptr(), nbytes, _stream())
     if status != KVM_OK:
         _check(status, "kvm_linear_prefill")
+    if given:
+        _count_write(given)
     if keep is not None:
         keep.append(ws)
     return out, state_out
@@ -768,10 +775,12 @@ def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, a
     cfg = _linear_config_of(B, Hq, Hkv, d, _io_of(q), _number(scale))
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out_ptr, writes = out.data_ptr(), (state,)
+    else:
+        out_ptr, writes = _want(out, (B, Hq, d), dt, dev, "out"), (state, out)
     ptrs = (_want(state, (B, Hkv, d, d), torch.float32, dev, "state"), _want(q, (B, Hq, d), dt, dev, "q"),
             _want(k, (B, Hkv, d), dt, dev, "k"), _want(v, (B, Hkv, d), dt, dev, "v"),
-            _want(log_decay, (Hkv,), torch.float32, dev, "log_decay"), _want(active, (B,), torch.int32, dev, "active"),
-            _want(out, (B, Hq, d), dt, dev, "out"))
+            _want(log_decay, (Hkv,), torch.float32, dev, "log_decay"), _want(active, (B,), torch.int32, dev, "active"), out_ptr)
     lib = _lib or load_library()
     if _current_device() == dev.index:
         status = lib.kvm_linear_decode(cfg, *ptrs, _raw_stream(dev.index))
@@ -780,6 +789,7 @@ def linear_decode(state, q, k, v, log_decay, *, scale: Optional[float] = None, a
             status = lib.kvm_linear_decode(cfg, *ptrs, _stream())
     if status != KVM_OK:
         _check(status, "kvm_linear_decode")
+    _count_write(writes)
     return out
 
 
@@ -812,6 +822,7 @@ def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: O
     if not 0 < Tq <= Tk:
         raise ValueError(f"q and k: want 0 < Tq <= Tk, got {Tq} and {Tk}")
     cfg = _window_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, _number(scale))
+    given = [t for t in (out, out_rest) if t is not None]
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     lse = torch.empty((B, Tq, Hq), dtype=torch.float32, device=dev) if want_lse else None
@@ -824,6 +835,8 @@ def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: O
         status = lib.kvm_window_prefill(cfg, *ptrs, Tq, Tk, _row_strides(q, k, v, out, lse), _stream())
     if status != KVM_OK:
         _check(status, "kvm_window_prefill")
+    if given:
+        _count_write(given)
     return (out, lse) if want_lse else out
 
 
@@ -877,6 +890,7 @@ def window_fill(cache_k, cache_v, k, v, *, window: int, n_sink: int = 0, lens=No
         status = lib.kvm_window_fill(cfg, *ptrs, T, _row_strides(k, k, v, k), _stream())
     if status != KVM_OK:
         _check(status, "kvm_window_fill")
+    _count_write((cache_k, cache_v))
 
 
 def window_decode(cache_k, cache_v, q, k, v, pos, *, window: int, n_sink: int = 0, scale: Optional[float] = None, out=None):
@@ -888,10 +902,13 @@ def window_decode(cache_k, cache_v, q, k, v, pos, *, window: int, n_sink: int = 
     cfg, nbytes = _window_token_config(B, Hq, Hkv, d, _io_of(q), window, n_sink, _number(scale))
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out_ptr, writes = out.data_ptr(), (cache_k, cache_v)
+    else:
+        out_ptr, writes = _want(out, (B, Hq, d), dt, dev, "out"), (cache_k, cache_v, out)
     rows = (B, Hkv, n_sink + window, d)
     ptrs = (_want(cache_k, rows, dt, dev, "cache_k"), _want(cache_v, rows, dt, dev, "cache_v"),
             _want(q, (B, Hq, d), dt, dev, "q"), _want(k, (B, Hkv, d), dt, dev, "k"), _want(v, (B, Hkv, d), dt, dev, "v"),
-            _want(pos, (B,), torch.int32, dev, "pos"), _want(out, (B, Hq, d), dt, dev, "out"))
+            _want(pos, (B,), torch.int32, dev, "pos"), out_ptr)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     lib = _lib or load_library()
     if _current_device() == dev.index:
@@ -901,4 +918,5 @@ def window_decode(cache_k, cache_v, q, k, v, pos, *, window: int, n_sink: int = 
             status = lib.kvm_window_decode(cfg, *ptrs, ws.data_ptr(), nbytes, _stream())
     if status != KVM_OK:
         _check(status, "kvm_window_decode")
+    _count_write(writes)
     return out

@@ -72,3 +72,63 @@ def test_the_backward_pass_has_the_forward_passs_sizes():
         w.fill_(30), s.fill_(0), c.fill_(0.125)
         for a, b in zip(want, torch.autograd.grad(out, leaves, x["dout"])):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T0", [40, 1500])   # (one segment and several)
+def test_a_state_advanced_before_the_backward_pass_is_noticed(T0):
+    """The backward pass reads the state that the call started from: advanced in place since, it is refused and not used."""
+    import paper_2605_09877_amd as kvm
+    gen = torch.Generator(DEV).manual_seed(0)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device=DEV)
+    q, k, v = (rnd(B, T0, h, D).requires_grad_() for h in (HQ, HKV, HKV))
+    x = inputs()
+    for advance in (lambda s: kvm.linear_decode(s, *token(x), x["ld"]),
+                    lambda s: kvm.linear_prefill(x["q"], x["k"], x["v"], x["ld"], state=s, state_out=s)):
+        state = x["state"].clone()
+        out, end = kvm.kvm_linear_attention(q, k, v, x["ld"], state=state)
+        want = torch.autograd.grad(out, (q, k, v), torch.ones_like(out), retain_graph=True)
+        advance(end.detach())   # (the end state is not read again)
+        again = torch.autograd.grad(out, (q, k, v), torch.ones_like(out), retain_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(want, again))
+        advance(state)
+        with pytest.raises(RuntimeError, match="inplace operation"):
+            torch.autograd.grad(out, (q, k, v), torch.ones_like(out))
+
+
+def test_what_a_call_writes_counts_as_written():
+    """Every tensor of the caller's that a call writes has another version afterwards; what it only reads has not."""
+    import paper_2605_09877_amd as kvm
+    x = inputs(torch.bfloat16)
+    qkv = [x[n] for n in "qkv"]
+    out, rest, one, end = torch.empty_like(x["q"]), torch.empty_like(x["q"]), torch.empty_like(x["q"][:, 0]).contiguous(), x["state"].clone()
+    ck, cv = kvm.window_cache(B, HKV, D, window=8, device=DEV)
+    pos = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    tok = token(x)
+    for call, writes in ((lambda: kvm.window_prefill(*qkv, window=8, out=out, out_rest=rest), (out, rest)),
+                         (lambda: kvm.window_fill(ck, cv, x["k"], x["v"], window=8), (ck, cv)),
+                         (lambda: kvm.window_decode(ck, cv, *tok, pos, window=8, out=one), (ck, cv, one)),
+                         (lambda: kvm.linear_prefill(*qkv, x["ld"], state=x["state"], out=out, state_out=end), (out, end)),
+                         (lambda: kvm.linear_decode(end, *tok, x["ld"], out=one), (end, one))):
+        every = [*qkv, *tok, x["ld"], x["state"], pos, ck, cv, out, rest, one, end]
+        before = [t._version for t in every]
+        call()
+        for t, n in zip(every, before):
+            assert (t._version > n) == any(t is w for w in writes)
+
+
+def test_tokens_in_inference_mode():
+    """States and caches made there have no version: the calls are the same."""
+    import paper_2605_09877_amd as kvm
+    x = inputs(torch.bfloat16)
+    tok, pos = token(x), torch.zeros(B, dtype=torch.int32, device=DEV)
+
+    def work():
+        state = x["state"].clone()
+        ck, cv = kvm.window_cache(B, HKV, D, window=8, device=DEV)
+        kvm.window_fill(ck, cv, x["k"], x["v"], window=8)
+        return kvm.linear_decode(state, *tok, x["ld"]), state, kvm.window_decode(ck, cv, *tok, pos + T, window=8), ck, cv
+
+    want = work()
+    with torch.inference_mode():
+        for a, b in zip(want, work()):
+            assert torch.equal(a, b)

@@ -132,3 +132,25 @@ def test_tokens_in_inference_mode():
     with torch.inference_mode():
         for a, b in zip(want, work()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Hq,Hkv,T", [(4, 1, 1), (1, 1, 1), (4, 4, 3)])
+def test_many_sequences_of_few_tokens(Hq, Hkv, T):
+    """2^18 sequences: no more workgroups are asked for than there are tiles of positions."""
+    import paper_2605_09877_amd as kvm
+    n = 1 << 18
+    gen = torch.Generator(DEV).manual_seed(0)
+    one = [torch.randn(8, T, h, D, generator=gen, device=DEV).bfloat16() for h in (Hq, Hkv, Hkv)]
+    q, k, v = (t.repeat(n // 8, 1, 1, 1).requires_grad_() for t in one)
+    out = kvm.kvm_window_attention(q, k, v, window=2)
+    grads = torch.autograd.grad(out, (q, k, v), out.detach())
+    for t in (out, *grads):   # the same eight sequences again and again
+        t = t.detach().unflatten(0, (n // 8, 8))
+        assert torch.equal(t, t[:1].expand_as(t))
+    few = [t.clone().requires_grad_() for t in one]
+    want = kvm.kvm_window_attention(*few, window=2)
+    # Eight sequences are another arrangement: P, dS and each result rounded once on either side, 2^-8 each, and where dP - D
+    # cancels (a token that sees itself alone) 128 roundings of 2^-24 of sums of up to 200, times scale |k| <= 1/2.
+    for got, ref in zip((out, *grads), (want, *torch.autograd.grad(want, few, want.detach()))):
+        assert torch.all((got[:8].float() - ref.float()).abs() <= 2.0 ** -5 * ref.float().abs().max() + 2.0 ** -9)
+    assert torch.equal(out[:8, 0], v[:8, 0].repeat_interleave(Hq // Hkv, 1))   # the first token sees itself alone

@@ -362,7 +362,7 @@ int kvm_prepare_qkv(const kvm_prep_params *p, const void *q_raw, const void *k_r
  * 0 .. Tk): keys behind are not looked at, queries behind get zeros and lse = -infinity.  In out, values that are not finite
  * reach the queries that see them and no others; a query all of whose logits are -infinity gets zeros.  In gradients they
  * also reach keys and queries of the same tiles (up to 128 positions).  Pointers are 16-byte aligned (lse: 4); outputs must
- * not overlap inputs. */
+ * not overlap inputs, and an output's strides must keep its rows apart from each other. */
 #define KVM_WINDOW_MAX_SINK 128
 typedef struct kvm_window_config {
   int32_t batch, n_q_heads, n_kv_heads, head_dim; /* d: 64 or 128; batch * n_q_heads < 2^24 */
@@ -412,7 +412,8 @@ int kvm_window_decode(const kvm_window_config *cfg, void *cache_k, void *cache_v
  * NaN where the recurrence makes it infinite or NaN.
  * lens: nullable device int32 [B], the tokens of each sequence of a padded batch (taken as 0 .. T): rows behind are
  * not looked at, their out is zero, and the state is the one at the sequence's own end.  Every pointer is 16-byte aligned;
- * outputs must not overlap inputs, except that state_out may be state_in itself. */
+ * outputs must not overlap inputs, except that state_out may be state_in itself, and out's strides must keep its rows apart from
+ * each other. */
 typedef struct kvm_linear_config {
   int32_t batch, n_q_heads, n_kv_heads, head_dim; /* d: 64 or 128; batch * n_q_heads < 2^24 */
   int32_t io_dtype;                                /* KVM_F32 | KVM_BF16 */

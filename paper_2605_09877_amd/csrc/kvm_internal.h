@@ -18,6 +18,25 @@ inline hipError_t allow_lds(OncePerDevice<hipError_t> &once, const void *kernel,
 // kvm_api.hip: keeps the text for kvm_last_hip_error; KVM_ERR_HIP.
 int report_hip(hipError_t e, const char *what);
 
+// Whether the rows of `width` elements that an output of three axes has are apart from each other: taken from the smallest stride to the
+// largest, each axis steps over all that the ones before it span.  (Axes of one entry are not stepped along.)
+inline bool rows_apart(const int64_t (&size)[3], const int64_t (&stride)[3], int64_t width) {
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j)
+      if (stride[order[j]] > stride[order[j + 1]]) {
+        const int x = order[j];
+        order[j] = order[j + 1];
+        order[j + 1] = x;
+      }
+  for (const int i : order) {
+    if (size[i] <= 1) continue;
+    if (stride[i] < width) return false;
+    width += (size[i] - 1) * stride[i];
+  }
+  return true;
+}
+
 // A strided source of per-token keys, values and merge gates for all units.
 // Element strides; the head_dim axis is contiguous.  Token index 0 is `k`'s first token.
 struct Src {

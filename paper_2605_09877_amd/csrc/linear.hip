@@ -638,7 +638,7 @@ extern "C" int kvm_linear_prefill(const kvm_linear_config *cfg, const void *q, c
     s.k_b = s.v_b = T * hk * d; s.k_t = s.v_t = hk * d; s.k_h = s.v_h = d;
   }
   if (!strides_ok(s.q_b, s.q_t, s.q_h, cfg) || !strides_ok(s.k_b, s.k_t, s.k_h, cfg) || !strides_ok(s.v_b, s.v_t, s.v_h, cfg) ||
-      !strides_ok(s.o_b, s.o_t, s.o_h, cfg))
+      !strides_ok(s.o_b, s.o_t, s.o_h, cfg) || !rows_apart({cfg->batch, T, hq}, {s.o_b, s.o_t, s.o_h}, d))
     return KVM_ERR_ARG;
   const Cut cut = cut_of(cfg, T);
   LinArgs a = {};

@@ -1512,9 +1512,10 @@ extern "C" int kvm_window_prefill(const kvm_window_config *cfg, const void *q, c
     s.lse_b = Tq * hq; s.lse_t = hq; s.lse_h = 1;
   }
   if (!strides_ok(s.q_b, s.q_t, s.q_h, cfg) || !strides_ok(s.k_b, s.k_t, s.k_h, cfg) || !strides_ok(s.v_b, s.v_t, s.v_h, cfg) ||
-      !strides_ok(s.o_b, s.o_t, s.o_h, cfg))
+      !strides_ok(s.o_b, s.o_t, s.o_h, cfg) || !rows_apart({cfg->batch, Tq, hq}, {s.o_b, s.o_t, s.o_h}, d))
     return KVM_ERR_ARG;
-  if (lse && (s.lse_b < 0 || s.lse_t < 1 || s.lse_h < 1)) return KVM_ERR_ARG;
+  if (lse && (s.lse_b < 0 || s.lse_t < 1 || s.lse_h < 1 || !rows_apart({cfg->batch, Tq, hq}, {s.lse_b, s.lse_t, s.lse_h}, 1)))
+    return KVM_ERR_ARG;
   WinArgs a = base_args(cfg, Tq, Tk, lens);
   a.q = (const char *)q; a.k = (const char *)k; a.v = (const char *)v; a.out = (char *)out; a.lse = lse;
   a.rest = es == 2 ? (char *)out_rest : nullptr;

@@ -154,3 +154,24 @@ def test_many_sequences_of_few_tokens(Hq, Hkv, T):
     for got, ref in zip((out, *grads), (want, *torch.autograd.grad(want, few, want.detach()))):
         assert torch.all((got[:8].float() - ref.float()).abs() <= 2.0 ** -5 * ref.float().abs().max() + 2.0 ** -9)
     assert torch.equal(out[:8, 0], v[:8, 0].repeat_interleave(Hq // Hkv, 1))   # the first token sees itself alone
+
+
+@pytest.mark.parametrize("order", [(0, 1, 2), (0, 2, 1), (2, 0, 1), (1, 2, 0), (1, 0, 2)], ids=str)
+def test_outputs_in_any_order_of_axes(order):
+    """[B, T, H] of out laid out in any order, with rows left out between; entries that share memory are refused."""
+    import paper_2605_09877_amd as kvm
+    x = inputs()
+    qkv = [x[n] for n in "qkv"]
+    shape = (B, 2 * T, HQ)
+    buf = torch.zeros(*(shape[i] for i in order), D, device=DEV).permute(*(order.index(i) for i in range(3)), 3)
+    out = buf[:, ::2]
+    for call in (lambda **kw: kvm.window_prefill(*qkv, window=8, **kw), lambda **kw: kvm.linear_prefill(*qkv, x["ld"], **kw)[0]):
+        want = call()
+        buf.zero_()
+        assert torch.equal(call(out=out), want) and torch.count_nonzero(buf[:, 1::2]) == 0
+        for bad in (torch.empty(1, T, HQ, D, device=DEV).expand(B, -1, -1, -1), torch.empty(B, T, 1, D, device=DEV).expand(-1, -1, HQ, -1),
+                    torch.empty(B * T * HQ * D, device=DEV).as_strided((B, T, HQ, D), (T * D, D, D, 1))):
+            with pytest.raises(kvm.KVMError):
+                call(out=bad)
+    only = torch.empty(1, T, HQ, D, device=DEV).as_strided((1, T, HQ, D), (0, HQ * D, D, 1))   # (an axis of one entry)
+    assert torch.equal(kvm.window_prefill(*(t[:1] for t in qkv), window=8, out=only), kvm.window_prefill(*(t[:1] for t in qkv), window=8))

@@ -56,8 +56,8 @@ struct WinArgs {
 
 // Keys of a tile.  With 32 the prompt kernel has registers for three workgroups to a compute unit, in whose turns the exponentials of one
 // run beside the products of another: 2 sequences of 16k tokens, 32 heads of 128 on 8, window 2048: 1094 us, 1147 with 64 and two
-// workgroups.  Rows of 64 channels, us, 32 / 64: 4 x 4k tokens, 16 heads on 4, 70 / 77; 2k, 16 heads, 15 / 20; 8 x 1000, 8 heads, 24 /
-// 21, the one kind that loses.  dq: 4 x 4k, 16 heads of 64 on 4, with dk and dv 207 / 216.
+// workgroups.  Rows of 64 channels, us, 32 / 64: 4 x 4k tokens, 16 heads on 4, 70 / 77; 2k, 16 heads, 15 / 20; 8 x 1000, 8 heads, 28 /
+// 26, the one kind that loses.  dq: 4 x 4k, 16 heads of 64 on 4, with dk and dv 207 / 216.
 constexpr int kTileRows = 32;
 
 __device__ __forceinline__ int tokens_of(const WinArgs &a, int b) {
@@ -1411,15 +1411,22 @@ size_t sums_bytes(const WinArgs &a, int d) {
 // Few workgroups for the device: 32 queries of one head in each instead, its waves sharing the key tiles.  Prompts, us, tiles shared / not
 // (workgroups not shared): 512 tokens, 8 heads 9 / 20 (32); 1000, 8 on 2 heads 13 / 33 (64); fp32, 777, 6 on 2 heads 12 / 35 (42);
 // 2048, 16 heads 55 / 66 (256); 1000, 32 on 8 heads, four to a workgroup, 28 / 26 (256); 4096, 16 on 4 heads 73 / 50 (512).
+// Of 64 units (sequence, KV head) and more, a grid as small has short rows: there only where the smaller workgroups run at once, two to a
+// compute unit, and had no tiles of a group's heads to share.  Shared / not (workgroups if shared): 64 x 128 tokens, one head, 6.8 /
+// 9.6 (256); 64 x 256, 10.1 / 13.5 (512); 100 x 160, 13.0 / 10.7 (520); 64 x 500, fp32, 76 / 67 (1024); 200 x 32 tokens, four heads on
+// one, 13.9 / 8.0 (800); 64 x 32, 6.6 / 7.2 (256).
 bool split_tiles(WinArgs &a) {
   const unsigned grid = query_grid(a);
   if (grid == 0 || grid >= (a.by_head ? 256u : 512u)) return false;
-  tile_queries(a, false, 32);
+  WinArgs b = a;
+  tile_queries(b, false, 32);
+  if ((int64_t)a.B * a.Hkv >= 64 && (a.by_head || query_grid(b) > 512)) return false;
+  a = b;
   return true;
 }
 // Prompts of a training step (lse is asked for) whose rows have few keys: the errors of dq and dk against a single rounding's are 1.43 to
 // 1.49 with P as one operand there (up to 1.56 for 16 tokens), 1.42 to 1.45 as two (1.49).  Beyond, the difference goes, and the second operand
-// costs: us, two / one, 64 x 256 tokens, 16 heads, 141 / 111; 4 x 4k, 16 heads of 64 on 4, window 128, 39 / 34; 2 x 256, 8 heads, 8.0 / 7.6.
+// costs: us, two / one, 64 x 256 tokens, 16 heads, 77 / 67; 4 x 4k, 16 heads of 64 on 4, window 128, 39 / 34; 2 x 256, 8 heads, 8.0 / 7.6.
 bool fine_rows(const WinArgs &a) { return a.lse && (a.Tk <= 256 || a.W + a.S <= 64); }
 
 template <typename T, int D, bool kFine>

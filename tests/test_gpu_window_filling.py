@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from oracle import mixers_oracle as mo
-from test_gpu_window import DEV, DT, f64, make, noise, out_bound, within
+from test_gpu_window import DEV, DT, f64, make, noise, out_bound, run_case, within
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +62,10 @@ def test_maxima_that_rise_or_fall_along_the_keys(io, d, step):
     for out in (kvm.window_prefill(*many, window=W, n_sink=S), kvm.window_prefill(*many, window=W, n_sink=S, want_lse=True)[0]):
         within(out[:1], ref, tol, "out")
         assert torch.equal(out, out[:1].expand_as(out))
+
+
+@pytest.mark.parametrize("io,d", [("bf16", 64), ("bf16", 128), ("f32", 128)])
+@pytest.mark.parametrize("B,T,Hq,Hkv", [(64, 120, 1, 1), (100, 160, 1, 1), (66, 33, 4, 1)])
+def test_many_short_rows(io, d, B, T, Hq, Hkv):
+    """Either side of the rule for 64 units and more: waves that share key tiles, and that do not (520 workgroups, a group's heads)."""
+    run_case(io, B, T, Hq, Hkv, d, window=50, n_sink=2, lens=[(23 * b) % (T + 1) for b in range(B - 1)] + [T])

@@ -190,6 +190,7 @@ __device__ __forceinline__ void attend_one_by_one(const WinArgs &a, const char *
     const float alpha = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(x - ref);
     m = m_new;
     l = fmaf(l, alpha, p);
+    if (l != l) break;   // (NaN stays, and makes out and lse NaN whatever follows)
 #pragma unroll
     for (int i = 0; i < 4 * DB; ++i) {
       float y[4];

@@ -658,14 +658,16 @@ def _heads(q: torch.Tensor, k: torch.Tensor, dims: int):
     return q.shape[-2], k.shape[-2], q.shape[-1]
 
 
+def _steps(t):
+    """The element strides of [B, T, H]; an axis of one entry has whatever stride torch left there, and is given one that rows have."""
+    stride, shape = t.stride(), t.shape
+    if 1 in shape[:3]:
+        return [n if size > 1 else shape[3] for n, size in zip(stride[:3], shape)]
+    return list(stride[:3])
+
+
 def _row_strides(q, k, v, out, lse=None) -> kvm_strides:
-    """Their element strides; an axis of one entry has whatever stride torch left there, and is given one that rows have."""
-    def of(t):
-        stride, shape = t.stride(), t.shape
-        if 1 in shape[:3]:
-            return [n if size > 1 else shape[3] for n, size in zip(stride[:3], shape)]
-        return stride[:3]
-    return kvm_strides(*of(q), *of(k), *of(v), *of(out), 0, 0, 0, *((0, 0, 0) if lse is None else lse.stride()))
+    return kvm_strides(*_steps(q), *_steps(k), *_steps(v), *_steps(out), 0, 0, 0, *((0, 0, 0) if lse is None else lse.stride()))
 
 
 def _number(scale) -> Optional[float]:
@@ -826,11 +828,11 @@ def window_prefill(q, k, v, *, window: int, n_sink: int = 0, lens=None, scale: O
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     lse = torch.empty((B, Tq, Hq), dtype=torch.float32, device=dev) if want_lse else None
-    if out_rest is not None and out_rest.stride() != out.stride():
-        raise ValueError("out_rest: want the strides of out")
     ptrs = [_want(q, q.shape, q.dtype, dev, "q", True), _want(k, (B, Tk, Hkv, d), q.dtype, dev, "k", True),
             _want(v, (B, Tk, Hkv, d), q.dtype, dev, "v", True), _want(lens, (B,), torch.int32, dev, "lens"),
             _want(out, q.shape, q.dtype, dev, "out", True), _want(out_rest, q.shape, q.dtype, dev, "out_rest", True), _ptr(lse)]
+    if out_rest is not None and _steps(out_rest) != _steps(out):
+        raise ValueError(f"out_rest: want the strides of out, got {out_rest.stride()} and {out.stride()}")
     with _on_device(dev):
         status = lib.kvm_window_prefill(cfg, *ptrs, Tq, Tk, _row_strides(q, k, v, out, lse), _stream())
     if status != KVM_OK:

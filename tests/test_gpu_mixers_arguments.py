@@ -175,3 +175,18 @@ def test_outputs_in_any_order_of_axes(order):
                 call(out=bad)
     only = torch.empty(1, T, HQ, D, device=DEV).as_strided((1, T, HQ, D), (0, HQ * D, D, 1))   # (an axis of one entry)
     assert torch.equal(kvm.window_prefill(*(t[:1] for t in qkv), window=8, out=only), kvm.window_prefill(*(t[:1] for t in qkv), window=8))
+
+
+def test_out_rest_of_an_axis_of_one_entry():
+    """Its stride, which may be anything, need not be out's; those of the other axes have to be."""
+    import paper_2605_09877_amd as kvm
+    x = inputs(torch.bfloat16)
+    qkv = [x[n][:1] for n in "qkv"]
+    wide = torch.zeros(3, T, HQ, D, dtype=torch.bfloat16, device=DEV)
+    out, rest = wide[1:2], torch.zeros(1, T, HQ, D, dtype=torch.bfloat16, device=DEV).as_strided((1, T, HQ, D), (D, HQ * D, D, 1))
+    want = torch.empty_like(qkv[0])
+    kvm.window_prefill(*qkv, window=8, out_rest=want)
+    assert kvm.window_prefill(*qkv, window=8, out=out, out_rest=rest) is out and torch.equal(rest, want) and torch.count_nonzero(rest)
+    for bad in (wide[:1, :, :1].expand(-1, -1, HQ, -1), wide[:1].transpose(1, 2), wide[:1, ::2], torch.zeros(1, T, 2 * HQ, D, device=DEV)[:, :, ::2]):
+        with pytest.raises(ValueError, match="out_rest"):
+            kvm.window_prefill(*qkv, window=8, out=out, out_rest=bad)

@@ -359,9 +359,11 @@ int kvm_prepare_qkv(const kvm_prep_params *p, const void *q_raw, const void *k_r
  * softmax of scale * q_t . k_j.  (The KVM layer's own window moves in blocks of C and has no keys that stay.)
  * Prompts: q, out [B, Tq, H_q, d]; k, v [B, Tk, H_kv, d]; query i stands at position i + Tk - Tq, so that a prompt may be given
  * in pieces with the keys before it.  lens: nullable device int32 [B], the keys of each sequence of a padded batch (taken as
- * 0 .. Tk): keys behind are not looked at, queries behind get zeros and lse = -infinity.  In out, values that are not finite
- * reach the queries that see them and no others; a query all of whose logits are -infinity gets zeros.  In gradients they
- * also reach keys and queries of the same tiles (up to 128 positions).  Pointers are 16-byte aligned (lse: 4); outputs must
+ * 0 .. Tk): keys behind are not looked at, queries behind get zeros and lse = -infinity (out_rest is not written there).  In
+ * out, of prompts and of tokens, values that are not finite reach the queries that see them and no others: a NaN in q or in a visible key
+ * makes out and lse NaN, one in a visible value its channel; a query all of whose logits are -infinity gets zeros.  In gradients
+ * they also reach keys and queries of the same tiles (up to 128 positions).  A call that takes 2^24 workgroups or more (filling
+ * caches of 64 GiB each, for one) is KVM_ERR_ARG.  Pointers are 16-byte aligned (lse: 4); outputs must
  * not overlap inputs, and an output's strides must keep its rows apart from each other. */
 #define KVM_WINDOW_MAX_SINK 128
 typedef struct kvm_window_config {

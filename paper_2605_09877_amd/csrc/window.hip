@@ -273,7 +273,7 @@ struct Fragments {
 // (fine_rows).  What P's rounding moves, lse and D = dout . out, moves every dS of a row: dq and dk of rows of n keys would have
 // the variance of 2 + 2 / n roundings instead of 2.
 // (fp32 rows of 128 channels: with two workgroups to a CU registers spill; 2 sequences of 4096 tokens of 16 heads, window 512,
-// take 399 us with one and 437 with two.)
+// take 385 us with one and 432 with two.)
 template <typename T, int D, bool kFine>
 __global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : kFine ? 2 : 3) void window_prefill_kernel(WinArgs a) {
   using Tl = Tile<T, D>;

@@ -10,7 +10,7 @@ from typing import Optional
 
 import torch
 
-from .binding import (KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, _number, _sizes, linear_backward, linear_prefill,
+from .binding import (KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, _number, _sizes, _steps, linear_backward, linear_prefill,
                       window_backward, window_prefill)
 
 
@@ -67,6 +67,19 @@ def _once(ctx) -> None:
         raise RuntimeError(f"{type(ctx).__name__}: the gradients are not differentiable again (create_graph)")
 
 
+def _gradient_wanted(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """t where the forward calls take it as it lies, a dense copy otherwise (broadcast heads, rows off 16-byte borders, ..)."""
+    if t.dim() != 4 or t.numel() == 0:
+        return t
+    (b, row, head), d, vec = _steps(t), t.shape[3], 16 // t.element_size()
+    apart = b % vec == row % vec == head % vec == 0 and head >= d and d <= row <= 1 << 23
+    return t if apart and t.stride(3) == 1 and t.data_ptr() % 16 == 0 else t.contiguous()
+
+
 class _LinearAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, log_decay, state, lens, scale):
@@ -98,6 +111,8 @@ def kvm_linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     The backward pass reads `state` again and raises an error if it has been advanced in place (linear_decode) since."""
     if log_decay.requires_grad:
         raise ValueError("log_decay: the decays are constants, they get no gradient")
+    if not _gradient_wanted(q, k, v, state):   # (the same bits, no copies of rows)
+        return linear_prefill(_rows(q), _rows(k), _rows(v), log_decay, state=state, lens=lens, scale=scale)
     return _LinearAttention.apply(q, k, v, log_decay, state, lens, _number(scale))
 
 
@@ -124,4 +139,6 @@ def kvm_window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, w
                          lens: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
     """Attention over the last `window` keys and the first `n_sink` ones, differentiable in q, k and v.  Shapes and lens as in
     window_prefill."""
+    if not _gradient_wanted(q, k, v):   # (the same bits, which follow lse being asked for, and neither copies of rows nor out_rest)
+        return window_prefill(_rows(q), _rows(k), _rows(v), window=window, n_sink=n_sink, lens=lens, scale=scale, want_lse=True)[0]
     return _WindowAttention.apply(q, k, v, *_sizes(window, n_sink), lens, _number(scale))

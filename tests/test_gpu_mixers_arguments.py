@@ -190,3 +190,53 @@ def test_out_rest_of_an_axis_of_one_entry():
     for bad in (wide[:1, :, :1].expand(-1, -1, HQ, -1), wide[:1].transpose(1, 2), wide[:1, ::2], torch.zeros(1, T, 2 * HQ, D, device=DEV)[:, :, ::2]):
         with pytest.raises(ValueError, match="out_rest"):
             kvm.window_prefill(*qkv, window=8, out=out, out_rest=bad)
+
+
+@pytest.mark.parametrize("T0", [40, 700])   # (P of the window as two operands and as one)
+def test_calls_whose_gradients_are_not_wanted(T0):
+    """The bits of a call whose gradients are, from views of a fused projection too; no memory but the results' and the workspace's."""
+    import paper_2605_09877_amd as kvm
+    gen = torch.Generator(DEV).manual_seed(0)
+    fused = torch.randn(4, T0, HQ + 2 * HKV, D, generator=gen, device=DEV).bfloat16()
+    ld = torch.tensor([-0.02, -0.3], device=DEV)
+    views = lambda t: t.split((HQ, HKV, HKV), 2)
+    size = 4 * T0 * HQ * D * 2
+    for call, results in ((lambda q, k, v: (kvm.kvm_window_attention(q, k, v, window=90, n_sink=3),), size + size // D * 2),
+                          (lambda q, k, v: kvm.kvm_linear_attention(q, k, v, ld), size + 4 * HKV * D * D * 4)):
+        want = call(*views(fused.clone().requires_grad_()))
+        assert all(t.requires_grad for t in want)
+        with torch.no_grad():
+            for q in (fused, fused.clone().requires_grad_()):
+                torch.cuda.synchronize()
+                torch.cuda.reset_peak_memory_stats()
+                before = torch.cuda.memory_allocated()
+                got = call(*views(q))
+                used = torch.cuda.max_memory_allocated() - before
+                assert all(torch.equal(a, b) and not b.requires_grad for a, b in zip(want, got))
+                workspace = 12 * 4 * HKV * D * D * 4 if len(got) == 2 and T0 > 40 else 256   # (start states of up to 12 segments)
+                assert used <= results + workspace + 8 * 512
+        assert not call(*views(fused))[0].requires_grad
+
+
+def test_any_layout_with_and_without_gradients():
+    """q, k and v that the forward calls do not take as they lie: broadcast heads and sequences, channels apart, rows off 16-byte borders."""
+    import paper_2605_09877_amd as kvm
+    x = inputs(torch.bfloat16)
+    off = torch.zeros(B * T * HKV * D + 8, dtype=torch.bfloat16, device=DEV)[1:1 + B * T * HKV * D].view(B, T, HKV, D)
+    wide = torch.zeros(B, T, HKV, D + 3, dtype=torch.bfloat16, device=DEV)[..., 3:]
+    apart = torch.zeros(B, T, D, HKV, dtype=torch.bfloat16, device=DEV).transpose(2, 3)
+    for t in (wide, apart):
+        t.copy_(x["k"])
+    for q, k, v in ((x["q"], x["k"][:, :, :1].expand(-1, -1, HKV, -1), x["v"]), (x["q"], x["k"][:1].expand(B, -1, -1, -1), x["v"][:1].expand(B, -1, -1, -1)),
+                    (x["q"], wide, x["v"]), (x["q"], apart, wide), (x["q"].transpose(0, 1).contiguous().transpose(0, 1), x["k"], x["v"]),
+                    (x["q"][:1, :1], x["k"][:1, :1, :1], apart[:1, :1, 1:])):
+        dense = [t.contiguous() for t in (q, k, v)]
+        for call in (lambda *a: kvm.kvm_window_attention(*a, window=9), lambda *a: kvm.kvm_linear_attention(*a, x["ld"][:a[1].shape[2]])[0]):
+            want = call(*dense)
+            assert torch.equal(call(q, k, v), want)
+            assert torch.equal(call(q, k.detach().requires_grad_(), v), want)
+    for call in (lambda k: kvm.kvm_window_attention(x["q"], k, x["v"], window=9), lambda k: kvm.kvm_linear_attention(x["q"], k, x["v"], x["ld"])):
+        with pytest.raises(kvm.KVMError):   # (dense, and off a 16-byte border: refused with gradients and without)
+            call(off)
+        with pytest.raises(kvm.KVMError):
+            call(off.detach().requires_grad_())

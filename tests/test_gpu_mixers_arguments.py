@@ -209,12 +209,12 @@ def test_calls_whose_gradients_are_not_wanted(T0):
             for q in (fused, fused.clone().requires_grad_()):
                 torch.cuda.synchronize()
                 torch.cuda.reset_peak_memory_stats()
-                before = torch.cuda.memory_allocated()
-                got = call(*views(q))
-                used = torch.cuda.max_memory_allocated() - before
+                before = torch.cuda.memory_stats()["requested_bytes.all.current"]
+                got = call(*views(q))   # (bytes as asked for: the allocator's blocks may be up to 1 MiB larger)
+                used = torch.cuda.memory_stats()["requested_bytes.all.peak"] - before
                 assert all(torch.equal(a, b) and not b.requires_grad for a, b in zip(want, got))
                 workspace = 12 * 4 * HKV * D * D * 4 if len(got) == 2 and T0 > 40 else 256   # (start states of up to 12 segments)
-                assert used <= results + workspace + 8 * 512
+                assert used <= results + workspace
         assert not call(*views(fused))[0].requires_grad
 
 

@@ -9,6 +9,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import (KVM_BF16, KVM_BUDGET_FIXED, KVM_F32, KVMState, _number, _sizes, _steps, linear_backward, linear_prefill,
                       window_backward, window_prefill)
@@ -68,7 +69,10 @@ def _once(ctx) -> None:
 
 
 def _gradient_wanted(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    """Also of tensors with tangents (forward mode), which autograd.Function refuses."""
+    tensors = [t for t in tensors if t is not None]
+    return torch.is_grad_enabled() and any(t.requires_grad for t in tensors) or (
+        forward_ad._current_level >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors))
 
 
 def _rows(t: torch.Tensor) -> torch.Tensor:

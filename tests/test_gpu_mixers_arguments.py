@@ -240,3 +240,17 @@ def test_any_layout_with_and_without_gradients():
             call(off)
         with pytest.raises(kvm.KVMError):
             call(off.detach().requires_grad_())
+
+
+def test_forward_mode_is_refused():
+    """Tangents are not dropped where no gradient is wanted otherwise."""
+    import paper_2605_09877_amd as kvm
+    from torch.autograd import forward_ad
+    x = inputs()
+    for grad in (True, False):
+        with torch.set_grad_enabled(grad), forward_ad.dual_level():
+            dual = forward_ad.make_dual(x["k"], x["k"])
+            for call in (lambda k: kvm.kvm_window_attention(x["q"], k, x["v"], window=8), lambda k: kvm.kvm_linear_attention(x["q"], k, x["v"], x["ld"])):
+                call(x["k"])
+                with pytest.raises(RuntimeError, match="jvp"):
+                    call(dual)
